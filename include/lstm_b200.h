@@ -376,6 +376,105 @@ LSTM_API int lstm_forward_noalloc(const float *wx, const float *wh, const float 
                          const float *x, int T, int B, const float *h0, const float *c0,
                          float *y, float *hT, float *cT, void *cuda_stream, char *err, int errlen);
 
+/* ---------------------------------------------------------------------------------------------------
+ * Operators of stacks of gated linear recurrences with 8-bit projections (the paper has no counterpart):
+ * a recurrence whose gates do not see h_{t-1}, so that whole sequences are scanned side by side; the norm in
+ * front of its projection; 8-bit storage; the projection.  They keep nothing between calls and own no memory:
+ *   - all matrices are DEVICE pointers of the caller, on the current device; calls are enqueued on cuda_stream,
+ *     allocate nothing, never synchronise and may be recorded into a CUDA graph.  Calls on several streams or
+ *     threads are independent of each other as long as their outputs and workspaces are.
+ *   - dtype is LSTM_F32 or LSTM_BF16, the type of the activations; states, scales, weights of the norm, biases
+ *     and sums are fp32; a result is rounded once, to the nearest.
+ *   - strides (..._t, ..._b, ..._ld) count elements; the last dimension is contiguous.  Pointers are aligned to
+ *     their elements.  Rows that are aligned to 16 bytes (widths of a multiple of 8) are read fastest.
+ *   - outputs must not overlap inputs or each other, but for hT over h0 (and dh0 over dhT).
+ *   - err (may be NULL): buffer of errlen bytes for the reason of a failure; nothing is launched then.
+ * ------------------------------------------------------------------------------------------------- */
+enum { LSTM_BF16 = 2 };                      /* dtype of the operators' activations, beside LSTM_F32 */
+
+/*
+ * Gated linear recurrence, for each batch row b and channel d, t in processing order (0..T-1, or with
+ * LSTM_LINREC_REVERSE from the sequence's last step to its first), h = h0 (or 0) in front of the first step:
+ *     with LSTM_LINREC_GATE   f = sigmoid(a_t)   h_t = f h_{t-1} + (1 - f) x_t       (a: logits)
+ *     without it              f = a_t            h_t = f h_{t-1} + x_t               (a: decays, |f| <= 1)
+ *   a, x, h: [T,B,D] with the strides given; h0, hT [B,D] fp32, contiguous, either may be NULL.
+ *   lengths: int32 [B] on the device, or NULL: sequence b has lengths[b] steps (held to 0..T); h is zero
+ *   behind them, and what a and x hold there is not used.  hT is the state behind the last step processed.
+ *   states: NULL, or fp32 [ceil(T / LSTM_LINREC_SEGMENT), B, D]: receives the state in front of processing step
+ *   LSTM_LINREC_SEGMENT * k (behind a sequence's end, its last state); the backward pass reads it.
+ * Decays above 1 are served as long as their product over the steps that count stays within the range of fp32.
+ * T = 1 is the serving step: with hT = h0 the state is updated in place.
+ */
+enum { LSTM_LINREC_GATE = 1, LSTM_LINREC_REVERSE = 2 };
+#define LSTM_LINREC_SEGMENT 16
+LSTM_API int lstm_linear_recurrence(const void *a, long long a_t, long long a_b, const void *x, long long x_t, long long x_b,
+                                    const float *h0, const int *lengths, int T, int B, int D, int dtype, int flags,
+                                    void *h, long long h_t, long long h_b, float *hT, float *states,
+                                    void *cuda_stream, char *err, int errlen);
+
+/*
+ * Its gradients.  dh [T,B,D] is the gradient that reaches h, dhT [B,D] fp32 (or NULL: 0) the one that reaches hT:
+ *     g_t = dh_t + f_{t+1} g_{t+1}     dx_t = (1 - f) g_t     da_t = g_t (h_{t-1} - x_t) f (1 - f)      (gate)
+ *                                      dx_t = g_t             da_t = g_t h_{t-1}                        (decay)
+ *     dh0 = f_1 g_1  [B,D] fp32, or NULL
+ * h is recomputed in fp32 from the forward call's states.  da and dx are zero behind a sequence's end, and what dh
+ * holds there is not used.
+ */
+LSTM_API int lstm_linear_recurrence_backward(const void *a, long long a_t, long long a_b, const void *x, long long x_t, long long x_b,
+                                             const float *states, const void *dh, long long dh_t, long long dh_b, const float *dhT,
+                                             const int *lengths, int T, int B, int D, int dtype, int flags,
+                                             void *da, long long da_t, long long da_b, void *dx, long long dx_t, long long dx_b,
+                                             float *dh0, void *cuda_stream, char *err, int errlen);
+
+/*
+ * Root-mean-square norm of rows, with the residual's addition in front:
+ *     r = x + residual (or x)         y = r / sqrt(mean(r^2) + eps) * w
+ * x, residual, r [rows, width] of dtype (residual and r may be NULL), w [width] fp32.  scales NULL: y [rows, width] of
+ * dtype.  scales not NULL: y holds e4m3 bytes (rows that start on 16 bytes) and scales [rows, ceil(width / 128)] as
+ * lstm_fp8_quantize with block_rows 1 makes them from the unrounded y.  y is computed from the unrounded sum.
+ * width <= LSTM_RMS_NORM_MAX_WIDTH, else LSTM_ERR_UNSUPPORTED.
+ */
+#define LSTM_RMS_NORM_MAX_WIDTH 16384
+LSTM_API int lstm_rms_norm(const void *x, long long x_ld, const void *residual, long long residual_ld, const float *w, float eps,
+                           int rows, int width, int dtype, void *y, long long y_ld, float *scales, void *r, long long r_ld,
+                           void *cuda_stream, char *err, int errlen);
+
+/*
+ * Its gradients at r (the stored sum; x where there was no residual), dy [rows, width] of dtype, dr the gradient that
+ * reaches r past the norm (or NULL):
+ *     dx = rstd (w dy - r rstd^2 mean(w dy r)) + dr        (the gradient of x and of residual alike)
+ *     dw = sum over rows of dy r rstd                      [width] fp32; the sums have one order, whatever the timing
+ * workspace: lstm_rms_norm_workspace(rows, width) floats that nothing else uses until the call has run (-1: bad sizes or
+ * no device).
+ */
+LSTM_API long long lstm_rms_norm_workspace(int rows, int width);
+LSTM_API int lstm_rms_norm_backward(const void *dy, long long dy_ld, const void *r, long long r_ld, const float *w, const void *dr,
+                                    long long dr_ld, float eps, int rows, int width, int dtype, void *dx, long long dx_ld, float *dw,
+                                    float *workspace, long long workspace_floats, void *cuda_stream, char *err, int errlen);
+
+/*
+ * 8-bit storage (e4m3) with fp32 scales: x ~ scale * q.  A scale belongs to 128 columns of one row (block_rows = 1,
+ * activations; scales [rows, ceil(width / 128)]) or to a block of 128 x 128 (block_rows = 128, weights;
+ * scales [ceil(rows / 128), ceil(width / 128)]); the last block of a row or column may be smaller.
+ *     scale = max |x| / 448 over the block, at least the smallest normal number;   q = x / scale, the nearest, ties to even
+ * A block that holds an infinity or a NaN gets that as its scale.  q rows start on 16 bytes (q and q_ld are multiples of
+ * 16); the bytes between width and q_ld are left as they are.
+ */
+LSTM_API int lstm_fp8_quantize(const void *x, long long x_ld, int rows, int width, int dtype, int block_rows, void *q, long long q_ld,
+                               float *scales, void *cuda_stream, char *err, int errlen);
+
+/*
+ * Product of such matrices, the input projection of a layer whose weights are held in 8 bits:
+ *     y[m,n] = sum_j sx[m,j] sw[n / 128, j] sum_{k in block j} qx[m,k] qw[n,k]  (+ bias[n])
+ * qx [rows, width] with sx of block_rows 1, qw [outs, width] with sw of block_rows 128 (rows start on 16 bytes),
+ * bias [outs] fp32 or NULL, y [rows, outs] of dtype.  Products run on the tensor cores (tcgen05, e4m3 operands); the sum
+ * of a block of 128 columns is scaled and added up in fp32.  A wait inside the kernel that gives up (which only a failed
+ * device can cause) leaves NaN in its tile of y.
+ */
+LSTM_API int lstm_fp8_product(const void *qx, long long qx_ld, const float *sx, const void *qw, long long qw_ld, const float *sw,
+                              const float *bias, int rows, int outs, int width, int dtype, void *y, long long y_ld,
+                              void *cuda_stream, char *err, int errlen);
+
 #ifdef __cplusplus
 }
 #endif

@@ -11,7 +11,8 @@ from pathlib import Path
 
 import numpy as np
 
-LSTM_F32, LSTM_BF16W_F32S = 0, 1
+LSTM_F32, LSTM_BF16W_F32S, LSTM_BF16 = 0, 1, 2
+LSTM_LINREC_GATE, LSTM_LINREC_REVERSE, LSTM_LINREC_SEGMENT, LSTM_RMS_NORM_MAX_WIDTH = 1, 2, 16, 16384
 LSTM_DENSE, LSTM_CSR = 0, 1
 LSTM_OK, LSTM_ERR_INVALID, LSTM_ERR_UNSUPPORTED, LSTM_ERR_CUDA, LSTM_ERR_NOMEM, LSTM_ERR_TIMEOUT, LSTM_ERR_INTERNAL = range(7)
 LSTM_K_STAGE, LSTM_K_PROJ, LSTM_K_RECUR, LSTM_K_COUNT = 0, 1, 2, 3
@@ -97,6 +98,22 @@ def load_library():
         lib.lstm_fold_input_affine.argtypes = [pf, pf, ci, ci, pf, pf, pf, pf]
         lib.lstm_csr_lane_layout.restype = ci
         lib.lstm_csr_lane_layout.argtypes = [vp, vp, vp, ci, ci, ci, ci, ci, vp, vp, pi, ctypes.POINTER(ctypes.c_longlong)]
+        ll, cf, text = ctypes.c_longlong, ctypes.c_float, [ctypes.c_char_p, ci]
+        lib.lstm_linear_recurrence.restype = ci
+        lib.lstm_linear_recurrence.argtypes = [vp, ll, ll, vp, ll, ll, vp, vp, ci, ci, ci, ci, ci, vp, ll, ll, vp, vp, vp, *text]
+        lib.lstm_linear_recurrence_backward.restype = ci
+        lib.lstm_linear_recurrence_backward.argtypes = [vp, ll, ll, vp, ll, ll, vp, vp, ll, ll, vp, vp, ci, ci, ci, ci, ci, vp, ll, ll,
+                                                        vp, ll, ll, vp, vp, *text]
+        lib.lstm_rms_norm.restype = ci
+        lib.lstm_rms_norm.argtypes = [vp, ll, vp, ll, vp, cf, ci, ci, ci, vp, ll, vp, vp, ll, vp, *text]
+        lib.lstm_rms_norm_workspace.restype = ll
+        lib.lstm_rms_norm_workspace.argtypes = [ci, ci]
+        lib.lstm_rms_norm_backward.restype = ci
+        lib.lstm_rms_norm_backward.argtypes = [vp, ll, vp, ll, vp, vp, ll, cf, ci, ci, ci, vp, ll, vp, vp, ll, vp, *text]
+        lib.lstm_fp8_quantize.restype = ci
+        lib.lstm_fp8_quantize.argtypes = [vp, ll, ci, ci, ci, ci, vp, ll, vp, vp, *text]
+        lib.lstm_fp8_product.restype = ci
+        lib.lstm_fp8_product.argtypes = [vp, ll, vp, vp, ll, vp, vp, ci, ci, ci, ci, vp, ll, vp, *text]
         _lib = lib
     return _lib
 
@@ -239,6 +256,50 @@ def lstm_forward_noalloc(wx, wh, b, in_dim, hidden, x, T, B, h0, c0, y, hT, cT, 
                                              h0 or None, c0 or None, y or None, hT or None, cT or None,
                                              stream or None, err, len(err))
     return rc, err.value.decode()
+
+
+# The operators: addresses as integers (0: not given), strides in elements.  They return (code, message).
+def _with_reason(fn, *args):
+    err = ctypes.create_string_buffer(160)
+    rc = fn(*args, err, 160)
+    return rc, err.value.decode() if rc else ""
+
+
+def lstm_linear_recurrence(a, a_t, a_b, x, x_t, x_b, h0, lengths, T, B, D, dtype, flags, h, h_t, h_b, hT, states, stream=0):
+    return _with_reason(load_library().lstm_linear_recurrence, a or None, a_t, a_b, x or None, x_t, x_b, h0 or None, lengths or None,
+                        T, B, D, dtype, flags, h or None, h_t, h_b, hT or None, states or None, stream or None)
+
+
+def lstm_linear_recurrence_backward(a, a_t, a_b, x, x_t, x_b, states, dh, dh_t, dh_b, dhT, lengths, T, B, D, dtype, flags,
+                                    da, da_t, da_b, dx, dx_t, dx_b, dh0, stream=0):
+    return _with_reason(load_library().lstm_linear_recurrence_backward, a or None, a_t, a_b, x or None, x_t, x_b, states or None,
+                        dh or None, dh_t, dh_b, dhT or None, lengths or None, T, B, D, dtype, flags, da or None, da_t, da_b,
+                        dx or None, dx_t, dx_b, dh0 or None, stream or None)
+
+
+def lstm_rms_norm(x, x_ld, residual, residual_ld, w, eps, rows, width, dtype, y, y_ld, scales, r, r_ld, stream=0):
+    return _with_reason(load_library().lstm_rms_norm, x or None, x_ld, residual or None, residual_ld, w or None, eps, rows, width, dtype,
+                        y or None, y_ld, scales or None, r or None, r_ld, stream or None)
+
+
+def lstm_rms_norm_workspace(rows, width):
+    """Floats of workspace that lstm_rms_norm_backward needs (-1: bad sizes or no device)."""
+    return load_library().lstm_rms_norm_workspace(rows, width)
+
+
+def lstm_rms_norm_backward(dy, dy_ld, r, r_ld, w, dr, dr_ld, eps, rows, width, dtype, dx, dx_ld, dw, workspace, workspace_floats, stream=0):
+    return _with_reason(load_library().lstm_rms_norm_backward, dy or None, dy_ld, r or None, r_ld, w or None, dr or None, dr_ld, eps, rows,
+                        width, dtype, dx or None, dx_ld, dw or None, workspace or None, workspace_floats, stream or None)
+
+
+def lstm_fp8_quantize(x, x_ld, rows, width, dtype, block_rows, q, q_ld, scales, stream=0):
+    return _with_reason(load_library().lstm_fp8_quantize, x or None, x_ld, rows, width, dtype, block_rows, q or None, q_ld, scales or None,
+                        stream or None)
+
+
+def lstm_fp8_product(qx, qx_ld, sx, qw, qw_ld, sw, bias, rows, outs, width, dtype, y, y_ld, stream=0):
+    return _with_reason(load_library().lstm_fp8_product, qx or None, qx_ld, sx or None, qw or None, qw_ld, sw or None, bias or None, rows, outs,
+                        width, dtype, y or None, y_ld, stream or None)
 
 
 # ---------------------------------------------------------------- convenience wrapper

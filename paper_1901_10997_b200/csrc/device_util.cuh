@@ -280,11 +280,11 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&v)[16])
 }
 
 // ---------------------------------------------------------------------------------------------------
-// Host: tensor map of a row-major bf16 matrix [rows][ld] of which `cols` columns are valid, boxes of
-// box_rows x 64 columns, 128-byte swizzle, zero fill outside.  The driver entry point is looked up through
+// Host: tensor map of a row-major matrix [rows][ld] of which `cols` columns are valid, boxes of
+// box_rows x 128 bytes, 128-byte swizzle, zero fill outside.  The driver entry point is looked up through
 // the runtime, so the library links against the runtime only.
 // ---------------------------------------------------------------------------------------------------
-inline bool encode_tmap_bf16_2d(void *map128, const void *base, long long rows, long long cols, long long ld, int box_rows)
+inline bool encode_tmap_2d(void *map128, CUtensorMapDataType type, int elem_bytes, const void *base, long long rows, long long cols, long long ld, int box_rows)
 {
     typedef CUresult (*EncodeFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
                                  const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
@@ -297,12 +297,16 @@ inline bool encode_tmap_bf16_2d(void *map128, const void *base, long long rows, 
         fn = (EncodeFn)p;
     }
     cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
-    cuuint64_t strides[1] = {(cuuint64_t)ld * 2};
-    cuuint32_t box[2] = {64u, (cuuint32_t)box_rows};
+    cuuint64_t strides[1] = {(cuuint64_t)ld * elem_bytes};
+    cuuint32_t box[2] = {128u / elem_bytes, (cuuint32_t)box_rows};
     cuuint32_t estr[2] = {1u, 1u};
-    return fn((CUtensorMap *)map128, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(base), dims, strides, box, estr,
+    return fn((CUtensorMap *)map128, type, 2, const_cast<void *>(base), dims, strides, box, estr,
               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+inline bool encode_tmap_bf16_2d(void *map128, const void *base, long long rows, long long cols, long long ld, int box_rows)
+{
+    return encode_tmap_2d(map128, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, base, rows, cols, ld, box_rows);
 }
 
 }  // namespace lstm

@@ -1,0 +1,138 @@
+// 8-bit values (e4m3) with a scale for each 128 columns of a row, or for each 128 x 128 block: the largest magnitude of a block
+// becomes 448, q = x / scale rounded to the nearest.  Bound by memory; every element is read once and stays in registers between
+// the maximum and the rounding.
+#include "../../include/lstm_b200.h"
+#include "row_parts.cuh"
+
+namespace lstm {
+namespace {
+
+struct QuantArgs {
+    const void *x;
+    long long x_ld;
+    int rows, width;
+    uint8_t *q;
+    long long q_ld;
+    float *scales;              // [ceil(rows / block rows)][ceil(width / 128)]
+};
+
+// a warp takes four strips of rows: enough loads in flight, and the strips of one row lie side by side
+constexpr int kStripsPerWarp = 4;
+template <typename T, int V>
+__global__ void __launch_bounds__(256) fp8_quantize_rows_kernel(const __grid_constant__ QuantArgs p)
+{
+    const int lane = threadIdx.x & 31;
+    const int strips = (p.width + kStrip - 1) / kStrip, blocks = (p.width + 127) / 128;
+    const long long all = (long long)p.rows * strips, at = ((long long)blockIdx.x * 8 + (threadIdx.x >> 5)) * kStripsPerWarp;
+    float x[kStripsPerWarp][8];
+#pragma unroll
+    for (int j = 0; j < kStripsPerWarp; ++j) {
+        const long long row = (at + j) / strips;
+        if (at + j < all) load_strip<T, V>((const T *)p.x + row * p.x_ld, (int)(at + j - row * strips) * kStrip, p.width, lane, x[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < kStripsPerWarp; ++j) {
+        if (at + j >= all) break;
+        const long long row = (at + j) / strips;
+        const int c0 = (int)(at + j - row * strips) * kStrip;
+        unsigned top[2];
+        strip_magnitudes<V>(x[j], lane, top);
+        const float s0 = block_scale(top[0]), s1 = block_scale(top[1]);
+        store_strip_e4m3<V>(p.q + row * p.q_ld, c0, p.width, lane, x[j], __fdiv_rn(1.0f, s0), __fdiv_rn(1.0f, s1));
+        float *out = p.scales + row * blocks + c0 / 128;
+        if (lane == 0) out[0] = s0;
+        if (lane == 16 && c0 + 128 < p.width) out[1] = s1;
+    }
+}
+
+// a CTA of 16 warps takes 128 rows of one strip (two blocks); a warp eight of the rows
+template <typename T, int V>
+__global__ void __launch_bounds__(512) fp8_quantize_blocks_kernel(const __grid_constant__ QuantArgs p)
+{
+    __shared__ unsigned tops[16][2];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int c0 = blockIdx.x * kStrip, blocks = (p.width + 127) / 128;
+    const long long r0 = (long long)blockIdx.y * 128 + warp * 8;
+    float x[8][8];
+    unsigned top[2] = {0u, 0u};
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        if (r0 + j < p.rows) load_strip<T, V>((const T *)p.x + (r0 + j) * p.x_ld, c0, p.width, lane, x[j]);
+        else
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[j][i] = 0.0f;
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        unsigned t[2];
+        strip_magnitudes<V>(x[j], lane, t);
+        top[0] = max(top[0], t[0]);
+        top[1] = max(top[1], t[1]);
+    }
+    if (lane == 0) tops[warp][0] = top[0];
+    if (lane == 16) tops[warp][1] = top[1];
+    __syncthreads();
+    top[0] = top[1] = 0u;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) { top[0] = max(top[0], tops[i][0]); top[1] = max(top[1], tops[i][1]); }
+    const float s0 = block_scale(top[0]), s1 = block_scale(top[1]);
+    const float i0 = __fdiv_rn(1.0f, s0), i1 = __fdiv_rn(1.0f, s1);
+    const float mine = V == 8 && lane >= 16 ? i1 : i0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        if (r0 + j < p.rows) store_strip_e4m3<V>(p.q + (r0 + j) * p.q_ld, c0, p.width, lane, x[j], mine, i1);
+    if (threadIdx.x == 0) {
+        float *out = p.scales + (long long)blockIdx.y * blocks + c0 / 128;
+        out[0] = s0;
+        if (c0 + 128 < p.width) out[1] = s1;
+    }
+}
+
+template <typename T, int V>
+void launch(const QuantArgs &p, int block_rows, cudaStream_t st)
+{
+    const long long strips = (p.width + kStrip - 1) / kStrip;
+    if (block_rows == 1)
+        fp8_quantize_rows_kernel<T, V><<<(unsigned)((p.rows * strips + 8 * kStripsPerWarp - 1) / (8 * kStripsPerWarp)), 256, 0, st>>>(p);
+    else
+        fp8_quantize_blocks_kernel<T, V><<<dim3((unsigned)strips, (unsigned)((p.rows + 127) / 128)), 512, 0, st>>>(p);
+}
+
+template <typename T>
+void by_vector(const QuantArgs &p, int v, int block_rows, cudaStream_t st)
+{
+    if (v == 8) launch<T, 8>(p, block_rows, st);
+    else if (v == 4) launch<T, 4>(p, block_rows, st);
+    else if (v == 2) launch<T, 2>(p, block_rows, st);
+    else launch<T, 1>(p, block_rows, st);
+}
+
+}  // namespace
+}  // namespace lstm
+
+using namespace lstm;
+
+extern "C" int lstm_fp8_quantize(const void *x, long long x_ld, int rows, int width, int dtype, int block_rows, void *q, long long q_ld,
+                                 float *scales, void *cuda_stream, char *err, int errlen)
+{
+    const Failure fail{err, errlen};
+    if (rows < 0 || width < 1) return fail(LSTM_ERR_INVALID, "bad argument: rows must be 0 or more, width 1 or more");
+    if (!known_type(dtype)) return fail(LSTM_ERR_INVALID, "bad argument: dtype must be LSTM_F32 or LSTM_BF16");
+    if (block_rows != 1 && block_rows != 128) return fail(LSTM_ERR_INVALID, "bad argument: block_rows must be 1 or 128");
+    if (rows == 0) return LSTM_OK;
+    if (!x || !q || !scales) return fail(LSTM_ERR_INVALID, "bad argument: x, q and scales must be given");
+    const int es = bytes_of(dtype);
+    if (!aligned_to(x, es) || !aligned_to(scales, 4)) return fail(LSTM_ERR_INVALID, "bad argument: a pointer is not aligned to its elements");
+    if (!aligned_to(q, 16) || q_ld % 16) return fail(LSTM_ERR_INVALID, "bad argument: 8-bit rows must start on 16 bytes");
+    if (block_rows == 128 && (rows + 127ll) / 128 > 65535) return fail(LSTM_ERR_UNSUPPORTED, "more than 65535 blocks of rows");
+    if (block_rows == 1 && (rows * ((width + 255ll) / 256) + 31) / 32 > 0x7fffffffll) return fail(LSTM_ERR_UNSUPPORTED, "too many blocks");
+    int sms = 0;
+    if (const int rc = device_sms(sms, fail)) return rc;
+    RowAlignment al(width);
+    al.matrix(x, x_ld, es);
+    QuantArgs p = {x, x_ld, rows, width, (uint8_t *)q, q_ld, scales};
+    if (dtype == LSTM_BF16) by_vector<__nv_bfloat16>(p, al.v, block_rows, (cudaStream_t)cuda_stream);
+    else by_vector<float>(p, al.v, block_rows, (cudaStream_t)cuda_stream);
+    const cudaError_t e = cudaGetLastError();
+    return e == cudaSuccess ? LSTM_OK : fail.cuda(e);
+}

@@ -1,0 +1,93 @@
+// What the stateless operators (linrec.cu, rms_norm.cu, fp8_quantize.cu, fp8_product.cu) share: failures at the C boundary,
+// the device's SM count, vectors of elements.
+#pragma once
+#include "device_util.cuh"
+
+#include <atomic>
+#include <cstdio>
+
+namespace lstm {
+
+// the reason of a failure, in the caller's buffer (which may be missing)
+struct Failure {
+    char *err;
+    int errlen;
+    int operator()(int code, const char *why) const
+    {
+        if (err && errlen > 0) snprintf(err, (size_t)errlen, "%s", why);
+        return code;
+    }
+    // a failed CUDA call; its error is not left behind for the next caller to find
+    int cuda(cudaError_t e) const
+    {
+        (void)cudaGetLastError();
+        return (*this)(LSTM_ERR_CUDA, cudaGetErrorString(e));
+    }
+};
+
+// SMs of the current device, which must run sm_100a code
+inline int device_sms(int &sms, const Failure &fail)
+{
+    static std::atomic<int> known[64];
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return fail.cuda(e);
+    if (dev >= 0 && dev < 64 && (sms = known[dev].load(std::memory_order_relaxed)) > 0) return LSTM_OK;
+    int major = 0;
+    if ((e = cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev)) != cudaSuccess) return fail.cuda(e);
+    if ((e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess) return fail.cuda(e);
+    if (major != 10) return fail(LSTM_ERR_CUDA, "the current device does not run sm_100a code");
+    if (dev >= 0 && dev < 64) known[dev].store(sms, std::memory_order_relaxed);
+    return LSTM_OK;
+}
+
+// ---------------------------------------------------------------------------------------------------
+// V elements of type T (float or __nv_bfloat16), loaded and stored as one word of up to 16 bytes
+// ---------------------------------------------------------------------------------------------------
+template <int BYTES> struct WordOf;
+template <> struct WordOf<2> { typedef unsigned short type; };
+template <> struct WordOf<4> { typedef unsigned type; };
+template <> struct WordOf<8> { typedef uint2 type; };
+template <> struct WordOf<16> { typedef uint4 type; };
+
+template <typename T, int V>
+struct alignas(sizeof(T) * V <= 16 ? sizeof(T) * V : 16) Vec { T e[V]; };
+
+template <typename T, int V>
+__device__ __forceinline__ Vec<T, V> load_vec(const T *p)
+{
+    constexpr int kBytes = sizeof(T) * V, kWord = kBytes <= 16 ? kBytes : 16;
+    typedef typename WordOf<kWord>::type W;
+    union { Vec<T, V> v; W w[kBytes / kWord]; } u;
+#pragma unroll
+    for (int i = 0; i < kBytes / kWord; ++i) u.w[i] = reinterpret_cast<const W *>(p)[i];
+    return u.v;
+}
+template <typename T, int V>
+__device__ __forceinline__ Vec<T, V> zero_vec()
+{
+    Vec<T, V> v;
+#pragma unroll
+    for (int i = 0; i < V; ++i) v.e[i] = T(0.0f);
+    return v;
+}
+template <typename T, int V>
+__device__ __forceinline__ float get(const Vec<T, V> &v, int i) { return static_cast<float>(v.e[i]); }
+
+template <typename T, int V>
+__device__ __forceinline__ void store_vec(T *p, const float (&o)[V])
+{
+    constexpr int kBytes = sizeof(T) * V, kWord = kBytes <= 16 ? kBytes : 16;
+    typedef typename WordOf<kWord>::type W;
+    union { Vec<T, V> v; W w[kBytes / kWord]; } u;
+#pragma unroll
+    for (int i = 0; i < V; ++i) u.v.e[i] = T(o[i]);      // rounds to nearest, ties to even
+#pragma unroll
+    for (int i = 0; i < kBytes / kWord; ++i) reinterpret_cast<W *>(p)[i] = u.w[i];
+}
+
+inline bool known_type(int dtype) { return dtype == LSTM_F32 || dtype == LSTM_BF16; }
+inline int bytes_of(int dtype) { return dtype == LSTM_BF16 ? 2 : 4; }
+inline bool aligned_to(const void *p, int bytes) { return (uintptr_t)p % (unsigned)bytes == 0; }
+
+}  // namespace lstm

@@ -1,0 +1,314 @@
+// Root-mean-square norm of rows, with the residual's addition in front and 8-bit values with scales behind where wanted:
+//
+//     r = x + residual        y = r rstd w        rstd = 1 / sqrt(mean(r^2) + eps)
+//
+// and its gradients  dx = rstd (w dy - r rstd^2 mean(w dy r)) + dr,   dw = sum over rows of dy r rstd.
+//
+// Bound by memory: a row is read once into the registers of one warp (up to 2048 columns) or of 4 or 8 warps, summed by shuffles,
+// and written once.  Sums are fp32 over at most 64 elements a lane before they are joined pairwise.
+#include "../../include/lstm_b200.h"
+#include "row_parts.cuh"
+
+namespace lstm {
+namespace {
+
+struct NormArgs {
+    const void *x, *residual;
+    long long x_ld, residual_ld;
+    const float *w;
+    float eps;
+    int rows, width;
+    void *y;
+    long long y_ld;
+    float *scales;              // not NULL: y is e4m3
+    void *r;
+    long long r_ld;
+};
+
+// sum over the WARPS warps that share a row; s holds two sets, used in turn
+template <int WARPS>
+__device__ __forceinline__ float row_sum(float v, float *s)
+{
+#pragma unroll
+    for (int o = 16; o > 0; o /= 2) v += __shfl_xor_sync(0xffffffffu, v, o);
+    if (WARPS == 1) return v;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    if (lane == 0) s[warp] = v;
+    __syncthreads();
+    v = 0.0f;
+#pragma unroll
+    for (int i = 0; i < WARPS; ++i) v += s[i];
+    return v;
+}
+
+// WARPS warps a row, NS strips a warp; rows of one warp stand four to a CTA
+template <typename T, int V, int WARPS, int NS>
+__global__ void __launch_bounds__(WARPS == 1 ? 128 : WARPS * 32) rms_norm_kernel(const __grid_constant__ NormArgs p)
+{
+    __shared__ float s[WARPS];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const long long row = WARPS == 1 ? (long long)blockIdx.x * 4 + warp : blockIdx.x;
+    if (row >= p.rows) return;                          // whole CTAs where warps meet
+    const int first = WARPS == 1 ? 0 : warp;
+    const T *x = (const T *)p.x + row * p.x_ld, *res = p.residual ? (const T *)p.residual + row * p.residual_ld : nullptr;
+    float r[NS][8], add[NS][8];
+#pragma unroll
+    for (int j = 0; j < NS; ++j) load_strip<T, V>(x, (first + j * WARPS) * kStrip, p.width, lane, r[j]);
+    if (res) {
+#pragma unroll
+        for (int j = 0; j < NS; ++j) load_strip<T, V>(res, (first + j * WARPS) * kStrip, p.width, lane, add[j]);
+#pragma unroll
+        for (int j = 0; j < NS; ++j)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) r[j][i] += add[j][i];
+    }
+    float sum = 0.0f;
+#pragma unroll
+    for (int j = 0; j < NS; ++j)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum = fmaf(r[j][i], r[j][i], sum);
+    sum = row_sum<WARPS>(sum, s);
+    const float rstd = 1.0f / sqrtf(sum / (float)p.width + p.eps);
+#pragma unroll
+    for (int j = 0; j < NS; ++j) {
+        const int c0 = (first + j * WARPS) * kStrip;
+        if (c0 >= p.width) break;
+        // the norm continues from the sum as it is, not from the rounded copy that is handed on: one rounding an output
+        if (p.r) store_strip<T, V>((T *)p.r + row * p.r_ld, c0, p.width, lane, r[j]);
+        float w[8], y[8];
+        load_strip<float, V>(p.w, c0, p.width, lane, w);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = r[j][i] * rstd * w[i];
+        if (!p.scales) {
+            store_strip<T, V>((T *)p.y + row * p.y_ld, c0, p.width, lane, y);
+            continue;
+        }
+        unsigned top[2];
+        strip_magnitudes<V>(y, lane, top);
+        const float s0 = block_scale(top[0]), s1 = block_scale(top[1]);
+        store_strip_e4m3<V>((uint8_t *)p.y + row * p.y_ld, c0, p.width, lane, y, __fdiv_rn(1.0f, s0), __fdiv_rn(1.0f, s1));
+        const int blocks = (p.width + 127) / 128;
+        float *out = p.scales + row * blocks + c0 / 128;
+        if (lane == 0) out[0] = s0;
+        if (lane == 16 && c0 + 128 < p.width) out[1] = s1;
+    }
+}
+
+struct NormBackArgs {
+    const void *dy, *r, *dr;
+    long long dy_ld, r_ld, dr_ld;
+    const float *w;
+    float eps;
+    int rows, width;
+    void *dx;
+    long long dx_ld;
+    float *part;                // [CTAs][width] partial sums of dw
+};
+
+// One CTA of WARPS warps walks over rows; a thread keeps its columns of w and of dw from row to row.
+template <typename T, int V, int WARPS, int NS>
+__global__ void __launch_bounds__(WARPS * 32) rms_norm_backward_kernel(const __grid_constant__ NormBackArgs p)
+{
+    __shared__ float2 s[2][WARPS];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    float dw[NS][8];
+#pragma unroll
+    for (int j = 0; j < NS; ++j)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) dw[j][i] = 0.0f;
+    int turn = 0;
+    for (long long row = blockIdx.x; row < p.rows; row += gridDim.x, turn ^= 1) {
+        const T *pr = (const T *)p.r + row * p.r_ld, *py = (const T *)p.dy + row * p.dy_ld;
+        float r[NS][8], dy[NS][8];
+#pragma unroll
+        for (int j = 0; j < NS; ++j) {
+            load_strip<T, V>(pr, (warp + j * WARPS) * kStrip, p.width, lane, r[j]);
+            load_strip<T, V>(py, (warp + j * WARPS) * kStrip, p.width, lane, dy[j]);
+        }
+        float rr = 0.0f, ry = 0.0f;
+#pragma unroll
+        for (int j = 0; j < NS; ++j) {
+            float w[8];
+            load_strip<float, V>(p.w, (warp + j * WARPS) * kStrip, p.width, lane, w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                rr = fmaf(r[j][i], r[j][i], rr);
+                ry = fmaf(r[j][i], w[i] * dy[j][i], ry);
+            }
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o /= 2) {
+            rr += __shfl_xor_sync(0xffffffffu, rr, o);
+            ry += __shfl_xor_sync(0xffffffffu, ry, o);
+        }
+        if (lane == 0) s[turn][warp] = make_float2(rr, ry);
+        __syncthreads();                                // the other set is read no more once all have come here
+        rr = ry = 0.0f;
+#pragma unroll
+        for (int i = 0; i < WARPS; ++i) { rr += s[turn][i].x; ry += s[turn][i].y; }
+        const float rstd = 1.0f / sqrtf(rr / (float)p.width + p.eps);
+        const float mean = ry / (float)p.width * rstd * rstd;
+#pragma unroll
+        for (int j = 0; j < NS; ++j) {
+            const int c0 = (warp + j * WARPS) * kStrip;
+            if (c0 >= p.width) break;
+            float w[8], o[8];
+            load_strip<float, V>(p.w, c0, p.width, lane, w);
+            float past[8];
+            if (p.dr) load_strip<T, V>((const T *)p.dr + row * p.dr_ld, c0, p.width, lane, past);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                dw[j][i] = fmaf(dy[j][i], r[j][i] * rstd, dw[j][i]);
+                o[i] = rstd * (w[i] * dy[j][i] - r[j][i] * mean);
+                if (p.dr) o[i] += past[i];
+            }
+            store_strip<T, V>((T *)p.dx + row * p.dx_ld, c0, p.width, lane, o);
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < NS; ++j)
+        store_strip<float, V>(p.part + (long long)blockIdx.x * p.width, (warp + j * WARPS) * kStrip, p.width, lane, dw[j]);
+}
+
+// dw = sum of the CTAs' rows, always in the same order: 32 columns a CTA, thread (column, i) adds rows i, i + 32, ...
+__global__ void __launch_bounds__(1024) rms_norm_join_kernel(const float *part, int parts, int width, float *dw)
+{
+    __shared__ float s[32][33];
+    const int c = blockIdx.x * 32 + threadIdx.x;
+    float sum = 0.0f;
+    if (c < width) {
+#pragma unroll 8
+        for (int i = threadIdx.y; i < parts; i += 32) sum += part[(long long)i * width + c];
+    }
+    s[threadIdx.y][threadIdx.x] = sum;
+    __syncthreads();
+    float v = s[threadIdx.x][threadIdx.y];
+#pragma unroll
+    for (int o = 16; o > 0; o /= 2) v += __shfl_xor_sync(0xffffffffu, v, o);
+    const int col = blockIdx.x * 32 + threadIdx.y;
+    if (threadIdx.x == 0 && col < width) dw[col] = v;
+}
+
+template <typename T, int V>
+void launch_norm(const NormArgs &p, cudaStream_t st)
+{
+    // one warp a row as far as its registers go (64 elements a lane), then 4 and 8 warps
+    if (p.width <= 512) rms_norm_kernel<T, V, 1, 2><<<(unsigned)((p.rows + 3ll) / 4), 128, 0, st>>>(p);
+    else if (p.width <= 2048) rms_norm_kernel<T, V, 1, 8><<<(unsigned)((p.rows + 3ll) / 4), 128, 0, st>>>(p);
+    else if (p.width <= 8192) rms_norm_kernel<T, V, 4, 8><<<p.rows, 128, 0, st>>>(p);
+    else rms_norm_kernel<T, V, 8, 8><<<p.rows, 256, 0, st>>>(p);
+}
+
+template <typename T, int V>
+void launch_back(const NormBackArgs &p, int parts, cudaStream_t st)
+{
+    if (p.width <= 1024) rms_norm_backward_kernel<T, V, 4, 1><<<parts, 128, 0, st>>>(p);
+    else if (p.width <= 2048) rms_norm_backward_kernel<T, V, 4, 2><<<parts, 128, 0, st>>>(p);
+    else if (p.width <= 4096) rms_norm_backward_kernel<T, V, 4, 4><<<parts, 128, 0, st>>>(p);
+    else if (p.width <= 8192) rms_norm_backward_kernel<T, V, 8, 4><<<parts, 256, 0, st>>>(p);
+    else rms_norm_backward_kernel<T, V, 16, 4><<<parts, 512, 0, st>>>(p);
+}
+
+// CTAs of the backward kernel, each of which leaves a row of partial sums
+int parts_of(int rows, int width, int sms)
+{
+    const int resident = width <= 4096 ? 6 : width <= 8192 ? 2 : 1;
+    return rows < sms * resident ? rows : sms * resident;
+}
+
+template <template <typename, int> class F, typename... A>
+void by_type(int dtype, int v, A &&...a)
+{
+    const bool half = dtype == LSTM_BF16;
+    if (v == 8) half ? F<__nv_bfloat16, 8>::go(a...) : F<float, 8>::go(a...);
+    else if (v == 4) half ? F<__nv_bfloat16, 4>::go(a...) : F<float, 4>::go(a...);
+    else if (v == 2) half ? F<__nv_bfloat16, 2>::go(a...) : F<float, 2>::go(a...);
+    else half ? F<__nv_bfloat16, 1>::go(a...) : F<float, 1>::go(a...);
+}
+template <typename T, int V> struct Forward { static void go(const NormArgs &p, cudaStream_t st) { launch_norm<T, V>(p, st); } };
+template <typename T, int V> struct Backward { static void go(const NormBackArgs &p, int parts, cudaStream_t st) { launch_back<T, V>(p, parts, st); } };
+
+int check(int rows, int width, int dtype, float eps, const Failure &fail)
+{
+    if (rows < 0 || width < 1) return fail(LSTM_ERR_INVALID, "bad argument: rows must be 0 or more, width 1 or more");
+    if (width > LSTM_RMS_NORM_MAX_WIDTH) return fail(LSTM_ERR_UNSUPPORTED, "rows of more than LSTM_RMS_NORM_MAX_WIDTH columns are not served");
+    if (!known_type(dtype)) return fail(LSTM_ERR_INVALID, "bad argument: dtype must be LSTM_F32 or LSTM_BF16");
+    if (!(eps >= 0.0f)) return fail(LSTM_ERR_INVALID, "bad argument: eps must be 0 or more");
+    return LSTM_OK;
+}
+
+}  // namespace
+}  // namespace lstm
+
+using namespace lstm;
+
+extern "C" {
+
+int lstm_rms_norm(const void *x, long long x_ld, const void *residual, long long residual_ld, const float *w, float eps, int rows, int width,
+                  int dtype, void *y, long long y_ld, float *scales, void *r, long long r_ld, void *cuda_stream, char *err, int errlen)
+{
+    const Failure fail{err, errlen};
+    if (const int rc = check(rows, width, dtype, eps, fail)) return rc;
+    if (rows == 0) return LSTM_OK;
+    if (!x || !w || !y) return fail(LSTM_ERR_INVALID, "bad argument: x, w and y must be given");
+    const int es = bytes_of(dtype);
+    if (!aligned_to(x, es) || !aligned_to(residual, es) || !aligned_to(r, es) || !aligned_to(w, 4) || !aligned_to(scales, 4) || (!scales && !aligned_to(y, es)))
+        return fail(LSTM_ERR_INVALID, "bad argument: a pointer is not aligned to its elements");
+    if (scales && (!aligned_to(y, 16) || y_ld % 16))
+        return fail(LSTM_ERR_INVALID, "bad argument: 8-bit rows must start on 16 bytes");
+    int sms = 0;
+    if (const int rc = device_sms(sms, fail)) return rc;
+    RowAlignment al(width);
+    al.matrix(x, x_ld, es);
+    al.matrix(residual, residual_ld, es);
+    al.matrix(r, r_ld, es);
+    al.matrix(w, 0, 4);
+    if (!scales) al.matrix(y, y_ld, es);
+    NormArgs p = {x, residual, x_ld, residual_ld, w, eps, rows, width, y, y_ld, scales, r, r_ld};
+    by_type<Forward>(dtype, al.v, p, (cudaStream_t)cuda_stream);
+    const cudaError_t e = cudaGetLastError();
+    return e == cudaSuccess ? LSTM_OK : fail.cuda(e);
+}
+
+int lstm_rms_norm_backward(const void *dy, long long dy_ld, const void *r, long long r_ld, const float *w, const void *dr, long long dr_ld,
+                           float eps, int rows, int width, int dtype, void *dx, long long dx_ld, float *dw, float *workspace,
+                           long long workspace_floats, void *cuda_stream, char *err, int errlen)
+{
+    const Failure fail{err, errlen};
+    if (const int rc = check(rows, width, dtype, eps, fail)) return rc;
+    if (!dw) return fail(LSTM_ERR_INVALID, "bad argument: dw must be given");
+    if (rows > 0 && (!dy || !r || !w || !dx)) return fail(LSTM_ERR_INVALID, "bad argument: dy, r, w and dx must be given");
+    const int es = bytes_of(dtype);
+    if (!aligned_to(dy, es) || !aligned_to(r, es) || !aligned_to(dr, es) || !aligned_to(dx, es) || !aligned_to(w, 4) || !aligned_to(dw, 4) ||
+        !aligned_to(workspace, 4))
+        return fail(LSTM_ERR_INVALID, "bad argument: a pointer is not aligned to its elements");
+    int sms = 0;
+    if (const int rc = device_sms(sms, fail)) return rc;
+    const cudaStream_t st = (cudaStream_t)cuda_stream;
+    const int parts = parts_of(rows, width, sms);
+    if (parts > 0 && (!workspace || workspace_floats < (long long)parts * width))
+        return fail(LSTM_ERR_INVALID, "bad argument: the workspace is smaller than lstm_rms_norm_workspace says");
+    if (parts > 0) {
+        RowAlignment al(width);
+        al.matrix(dy, dy_ld, es);
+        al.matrix(r, r_ld, es);
+        al.matrix(dr, dr_ld, es);
+        al.matrix(dx, dx_ld, es);
+        al.matrix(w, 0, 4);
+        al.matrix(workspace, 0, 4);
+        NormBackArgs p = {dy, r, dr, dy_ld, r_ld, dr_ld, w, eps, rows, width, dx, dx_ld, workspace};
+        by_type<Backward>(dtype, al.v, p, parts, st);
+    }
+    rms_norm_join_kernel<<<(width + 31) / 32, dim3(32, 32), 0, st>>>(workspace, parts, width, dw);
+    const cudaError_t e = cudaGetLastError();
+    return e == cudaSuccess ? LSTM_OK : fail.cuda(e);
+}
+
+long long lstm_rms_norm_workspace(int rows, int width)
+{
+    int sms = 0;
+    if (rows < 0 || width < 1 || width > LSTM_RMS_NORM_MAX_WIDTH || device_sms(sms, Failure{nullptr, 0}) != LSTM_OK) return -1;
+    return (long long)parts_of(rows, width, sms) * width;
+}
+
+}  // extern "C"

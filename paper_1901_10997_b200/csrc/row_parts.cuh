@@ -1,0 +1,119 @@
+// Rows of a matrix in the registers of a warp: the unit is a strip of 256 columns, 8 elements a lane, of which lane l holds
+// 8 / V vectors of V neighbours (vector q: columns q * 32 V + l V).  V follows the alignment of the rows, so that every access of a
+// warp is one run of memory whatever it is; a block of 128 columns lies in one warp for every V.
+#pragma once
+#include "operators.cuh"
+
+#include <cuda_fp8.h>
+
+namespace lstm {
+
+constexpr int kStrip = 256;
+constexpr float kE4m3Max = 448.0f;
+
+template <int V>
+__device__ __forceinline__ int strip_col(int q, int lane) { return q * 32 * V + lane * V; }
+
+// lane's 8 elements of the strip at column c0; columns behind `width` read as zero
+template <typename T, int V>
+__device__ __forceinline__ void load_strip(const T *row, int c0, int width, int lane, float (&o)[8])
+{
+#pragma unroll
+    for (int q = 0; q < 8 / V; ++q) {
+        const int c = c0 + strip_col<V>(q, lane);
+        const Vec<T, V> v = c < width ? load_vec<T, V>(row + c) : zero_vec<T, V>();
+#pragma unroll
+        for (int i = 0; i < V; ++i) o[q * V + i] = get<T, V>(v, i);
+    }
+}
+template <typename T, int V>
+__device__ __forceinline__ void store_strip(T *row, int c0, int width, int lane, const float (&o)[8])
+{
+#pragma unroll
+    for (int q = 0; q < 8 / V; ++q) {
+        const int c = c0 + strip_col<V>(q, lane);
+        float e[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) e[i] = o[q * V + i];
+        if (c < width) store_vec<T, V>(row + c, e);
+    }
+}
+
+// |x| as an integer of the same order, in which NaN is above infinity
+__device__ __forceinline__ unsigned magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+
+// The scale of a block from its largest magnitude.  Blocks of zeros (and those whose scale would be subnormal) get the smallest
+// normal number, so that its reciprocal is finite; a block that holds an infinity or NaN gets that as its scale.
+__device__ __forceinline__ float block_scale(unsigned largest)
+{
+    const unsigned least = 0x04e00000u;                 // 448 * 2^-126
+    return __fdiv_rn(__uint_as_float(max(largest, least)), kE4m3Max);
+}
+// four values as e4m3, the nearest, at most 448 in magnitude
+__device__ __forceinline__ unsigned to_e4m3x2(float a, float b)
+{
+    return __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
+}
+
+// largest magnitude of the lane's elements in block `half` of the strip, over the lanes that share the block
+template <int V>
+__device__ __forceinline__ void strip_magnitudes(const float (&y)[8], int lane, unsigned (&top)[2])
+{
+    top[0] = top[1] = 0u;
+    if (V == 8) {                                       // a lane is in one block: lanes 0-15 the first, 16-31 the second
+#pragma unroll
+        for (int i = 0; i < 8; ++i) top[0] = max(top[0], magnitude(y[i]));
+#pragma unroll
+        for (int o = 1; o < 16; o *= 2) top[0] = max(top[0], __shfl_xor_sync(0xffffffffu, top[0], o));
+        top[1] = top[0];                                // each lane's own block in both places
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            top[0] = max(top[0], magnitude(y[i]));
+            top[1] = max(top[1], magnitude(y[4 + i]));
+        }
+        top[0] = __reduce_max_sync(0xffffffffu, top[0]);
+        top[1] = __reduce_max_sync(0xffffffffu, top[1]);
+    }
+}
+
+// the lane's 8 elements, divided by their blocks' scales, as e4m3 bytes
+template <int V>
+__device__ __forceinline__ void store_strip_e4m3(uint8_t *row, int c0, int width, int lane, const float (&y)[8], float inv0, float inv1)
+{
+#pragma unroll
+    for (int q = 0; q < 8 / V; ++q) {
+        const int c = c0 + strip_col<V>(q, lane);
+        if (c >= width) continue;
+        const float inv = V == 8 ? inv0 : q * V < 4 ? inv0 : inv1;
+        unsigned w[V == 8 ? 2 : 1];
+        if (V == 1) {
+            w[0] = to_e4m3x2(y[q] * inv, 0.0f);
+            row[c] = (uint8_t)w[0];
+        } else if (V == 2) {
+            w[0] = to_e4m3x2(y[2 * q] * inv, y[2 * q + 1] * inv);
+            *reinterpret_cast<unsigned short *>(row + c) = (unsigned short)w[0];
+        } else {
+#pragma unroll
+            for (int i = 0; i < V / 4; ++i)
+                w[i] = to_e4m3x2(y[q * V + 4 * i] * inv, y[q * V + 4 * i + 1] * inv) |
+                       to_e4m3x2(y[q * V + 4 * i + 2] * inv, y[q * V + 4 * i + 3] * inv) << 16;
+            if (V == 4) *reinterpret_cast<unsigned *>(row + c) = w[0];
+            if (V == 8) *reinterpret_cast<uint2 *>(row + c) = make_uint2(w[0], w[V == 8 ? 1 : 0]);
+        }
+    }
+}
+
+// widest vector (8, 4, 2 or 1 elements) that divides the width and to which every matrix's rows are aligned
+struct RowAlignment {
+    int v;
+    explicit RowAlignment(int width) : v(8) { while (width % v) v /= 2; }
+    void matrix(const void *p, long long ld, int bytes)
+    {
+        if (!p) return;
+        auto fits = [&](int n) { const int word = n * bytes < 16 ? n * bytes : 16; return (uintptr_t)p % word == 0 && ld * bytes % word == 0; };
+        while (v > 1 && !fits(v)) v /= 2;
+    }
+};
+
+}  // namespace lstm
