@@ -5,15 +5,16 @@
 // The LSTM's cell with gates that do not see h_{t-1}: a step is the affine map h -> f h + b, maps compose to maps,
 // (A2, H2) o (A1, H1) = (A2 A1, A2 H1 + H2), so spans of steps are reduced side by side and joined afterwards.
 //
-// A thread owns 16 consecutive steps of one vector of channels.  It loads them all at once (that is what keeps enough bytes
-// in flight), reduces them to one map in registers, learns the state in front of its steps and runs through them once more
-// from registers: inputs are read once and outputs written once.  Maps are joined in shared memory within a CTA and through
-// distributed shared memory within a cluster of up to 16 CTAs that cover consecutive spans of time; one cluster barrier per
-// 16 x CTAs x segments steps, no flags, no workspace, and an order of sums that does not depend on timing.
+// A thread owns 8 or 16 consecutive steps of a vector of up to four channels.  It reduces them to one map in registers, learns the
+// state in front of its steps and runs through them once more from registers: inputs are read once and outputs written once.
+// Maps are joined by shuffles within a warp, in shared memory within a CTA and through distributed shared memory within a cluster
+// whose CTAs cover consecutive spans of time: no flags in global memory, no workspace, and an order of sums that does not
+// depend on timing.  Inputs come two spans ahead of their use by asynchronous copies into places of the thread's own in shared
+// memory, so that neither the joining nor a barrier holds them up.
 // State, maps and gates are fp32 throughout; outputs are rounded once.
 //
 // Backward: g_t = dh_t + f_{t+1} g_{t+1} is the same recurrence from the other end.  h is not read back: the forward pass
-// leaves the fp32 state in front of every 16th step, and a thread recomputes its own 16 from there (1/4 byte an element
+// leaves the fp32 state in front of every 16th step, and its steps are run through again from there (1/4 byte an element
 // instead of two for a rounded h, and h - x does not lose digits to that rounding).
 #include "../../include/lstm_b200.h"
 #include "operators.cuh"
@@ -21,8 +22,18 @@
 namespace lstm {
 namespace {
 
-constexpr int kSeg = LSTM_LINREC_SEGMENT;   // steps per thread
-constexpr int kThreads = 128;               // 3 to 4 CTAs an SM at 128 to 168 registers a thread
+constexpr int kThreads = 128;
+constexpr int kMaxCluster = 16;
+
+// How a warp's lanes are laid out for vectors of V channels: 32 channels side by side, and V spans of time.
+template <int V>
+struct Lay {
+    static constexpr int kLanes = 32 / V;                   // vectors side by side
+    static constexpr int kSpans = V;                        // spans of a warp, one behind the other
+    static constexpr int kSteps = V == 1 ? 16 : 8;          // steps of a span
+    static constexpr int kWarpSteps = kSpans * kSteps;      // a multiple of the 16 steps between saved states
+    static_assert(kWarpSteps % LSTM_LINREC_SEGMENT == 0 && LSTM_LINREC_SEGMENT == 16, "a warp begins at a saved state");
+};
 
 struct LinrecArgs {
     const void *a, *x;
@@ -42,32 +53,42 @@ struct LinrecArgs {
     long long da_t, da_b;
 };
 
+__device__ __forceinline__ float rcp_fast(float x)
+{
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
 // f and 1 - f, both to full relative accuracy: with e = exp(-|u|) they are 1/(1+e) and e/(1+e), in the order that the sign says.
 // bf16 data: the hardware's exponential (error 2^-22 and |u| 2^-24) is far inside a rounding to 8 bits; fp32 data: expf.
 template <typename T>
 __device__ __forceinline__ void gate_pair(float u, float &f, float &w)
 {
-    const float m = -fabsf(u);
-    const float e = sizeof(T) == 2 ? ex2_fast(1.4426950408889634f * m) : expf(m);
-    const float s = __fdividef(1.0f, 1.0f + e), r = e * s;
+    const float e = sizeof(T) == 2 ? ex2_fast(-1.4426950408889634f * fabsf(u)) : expf(-fabsf(u));
+    const float s = rcp_fast(1.0f + e), r = e * s;
     f = u >= 0.0f ? s : r;
     w = u >= 0.0f ? r : s;
 }
-
-// h behind a map; a state of zero stays out of it, whatever the product of the decays grew to
-__device__ __forceinline__ float apply_map(float A, float H, float h) { return h == 0.0f ? H : fmaf(A, h, H); }
 
 template <int V>
 struct alignas(8 * V) Map { float A[V], H[V]; };
 
 template <int V>
-__device__ __forceinline__ void join_behind(Map<V> &m, const Map<V> &later)      // m := later o m
+__device__ __forceinline__ void apply(const Map<V> &m, float (&h)[V])
 {
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-        m.H[v] = apply_map(later.A[v], later.H[v], m.H[v]);
-        m.A[v] *= later.A[v];
-    }
+    for (int v = 0; v < V; ++v) h[v] = fmaf(m.A[v], h[v], m.H[v]);
+}
+// m := later o m.  A product of decays that grew out of range is held at its edge: a state of zero stays zero behind it.
+template <int V, bool GATE>
+__device__ __forceinline__ float held(float A) { return GATE ? A : fmaxf(-3.4028235e38f, fminf(3.4028235e38f, A)); }
+template <int V, bool GATE>
+__device__ __forceinline__ void join_behind(Map<V> &m, const Map<V> &later)
+{
+    apply<V>(later, m.H);
+#pragma unroll
+    for (int v = 0; v < V; ++v) m.A[v] = held<V, GATE>(m.A[v] * later.A[v]);
 }
 
 __device__ __forceinline__ uint32_t cluster_rank()
@@ -76,293 +97,512 @@ __device__ __forceinline__ uint32_t cluster_rank()
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
     return r;
 }
+__device__ __forceinline__ uint32_t at_rank(uint32_t smem_addr, uint32_t rank)
+{
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_addr), "r"(rank));
+    return r;
+}
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
-// Shared by both directions: the joining of the threads' maps.
-template <int V, int LX>
+// V floats to another CTA's shared memory, counted by its barrier
+template <int V>
+__device__ __forceinline__ void send(uint32_t to, const float (&v)[V], uint32_t bar)
+{
+    if (V == 4)
+        asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];"
+                     ::"r"(to), "f"(v[0]), "f"(v[V > 1 ? 1 : 0]), "f"(v[V > 2 ? 2 : 0]), "f"(v[V > 3 ? 3 : 0]), "r"(bar) : "memory");
+    else if (V == 2)
+        asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];"
+                     ::"r"(to), "f"(v[0]), "f"(v[V > 1 ? 1 : 0]), "r"(bar) : "memory");
+    else
+        asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.f32 [%0], %1, [%2];" ::"r"(to), "f"(v[0]), "r"(bar) : "memory");
+}
+
+// ---------------------------------------------------------------------------------------------------
+// The joining of the threads' maps, the same in both directions.  Every thread holds the carry of its channels: the state in front
+// of the spans that the cluster is working on.  `order` counts a warp's spans in the order in which they are joined.
+// ---------------------------------------------------------------------------------------------------
+template <int V, bool GATE>
 struct Joiner {
-    static constexpr int kSegsPerWarp = 32 / LX;
+    typedef Lay<V> L;
     struct Shared {
-        Map<V> warp[2][kThreads / 32][LX];
-        Map<V> cta[2][16][LX];
+        Map<V> warp[2][kThreads / 32][L::kLanes];
+        Map<V> cta[2][kMaxCluster][L::kLanes];
+        alignas(8) unsigned long long bar[2];
+        int gave_up;
     };
-    // in: the thread's map and the carry in front of this span; out: the state in front of the thread, the carry behind the span
-    static __device__ __forceinline__ void join(Shared &s, int parity, const Map<V> &mine, int csize, int rank, float (&carry)[V], float (&before)[V])
+    Shared &s;
+    const int csize, rank, c, order, warp, nwarps;
+    int turn = 0;               // joinings so far; the two sets of shared memory are used in turn
+
+    __device__ Joiner(Shared &s_, int csize_)
+        : s(s_), csize(csize_), rank(csize_ > 1 ? (int)cluster_rank() : 0), c(threadIdx.x % L::kLanes), order(threadIdx.x % 32 / L::kLanes),
+          warp(threadIdx.x / 32), nwarps(blockDim.x / 32)
     {
-        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = lane % LX, nwarps = blockDim.x >> 5;
-        Map<V> m = mine;                // inclusive over the warp's segments
+        if (csize == 1) return;
+        if (threadIdx.x == 0) {
+            s.gave_up = 0;
+            mbar_init(smem_u32(&s.bar[0]), 1);
+            mbar_init(smem_u32(&s.bar[1]), 1);
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        }
+        cluster_arrive();       // waited for in ready(): the others' barriers stand before anything is sent to them
+    }
+    __device__ void ready() const { if (csize > 1) cluster_wait(); }
+    __device__ void leave() const
+    {
+        if (csize > 1) { cluster_arrive(); cluster_wait(); }
+    }
+
+    // mine: the thread's map; carry: in front of these spans -> behind them; before: the state in front of the thread's steps
+    __device__ __forceinline__ void join(const Map<V> &mine, float (&carry)[V], float (&before)[V])
+    {
+        const int set = turn & 1;
+        Map<V> upto = mine;             // the warp's spans up to this one
 #pragma unroll
-        for (int o = LX; o < 32; o *= 2) {
+        for (int o = 1; o < L::kSpans; o *= 2) {
             Map<V> e;
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                e.A[v] = __shfl_up_sync(0xffffffffu, m.A[v], o);
-                e.H[v] = __shfl_up_sync(0xffffffffu, m.H[v], o);
+                e.A[v] = __shfl_up_sync(0xffffffffu, upto.A[v], o * L::kLanes);
+                e.H[v] = __shfl_up_sync(0xffffffffu, upto.H[v], o * L::kLanes);
             }
-            if (lane >= o) {
-                join_behind<V>(e, m);
-                m = e;
+            if (order >= o) {
+                join_behind<V, GATE>(e, upto);
+                upto = e;
             }
         }
-        if (lane >= 32 - LX) s.warp[parity][warp][c] = m;
-        Map<V> pre;                     // exclusive over the warp's segments
-#pragma unroll
-        for (int v = 0; v < V; ++v) { pre.A[v] = 1.0f; pre.H[v] = 0.0f; }
-        if (LX < 32) {
-            Map<V> e;
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                e.A[v] = __shfl_up_sync(0xffffffffu, m.A[v], LX % 32);
-                e.H[v] = __shfl_up_sync(0xffffffffu, m.H[v], LX % 32);
-            }
-            if (lane >= LX) pre = e;
-        }
+        if (order == L::kSpans - 1) s.warp[set][warp][c] = upto;
         __syncthreads();
-        Map<V> front, all;              // of the CTA's warps: those in front of this one, all of them
-#pragma unroll
-        for (int v = 0; v < V; ++v) { all.A[v] = 1.0f; all.H[v] = 0.0f; }
-        front = all;
-        for (int w = 0; w < nwarps; ++w) {
-            if (w == warp) front = all;
-            join_behind<V>(all, s.warp[parity][w][c]);
-        }
         float h[V];
         if (csize > 1) {
-            if (threadIdx.x < LX) {
-                const uint32_t mine_at = (uint32_t)__cvta_generic_to_shared(&s.cta[parity][rank][c]);
-                for (int r = 0; r < csize; ++r) {
-                    uint32_t there;
-                    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(mine_at), "r"(r));
-#pragma unroll
-                    for (int v = 0; v < V; ++v) {
-                        asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(there + 4 * v), "f"(all.A[v]) : "memory");
-                        asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(there + 4 * (V + v)), "f"(all.H[v]) : "memory");
-                    }
+            const uint32_t bar = smem_u32(&s.bar[set]);
+            if (warp == 0) {            // the CTA's map goes to all CTAs of the cluster
+                if (threadIdx.x == 0) mbar_expect_tx(bar, csize * L::kLanes * (int)sizeof(Map<V>));
+                Map<V> all = s.warp[set][0][c];
+                for (int w = 1; w < nwarps; ++w) join_behind<V, GATE>(all, s.warp[set][w][c]);
+                const uint32_t slot = smem_u32(&s.cta[set][rank][c]);
+                for (int r = order; r < csize; r += L::kSpans) {
+                    const uint32_t to = at_rank(slot, r), their = at_rank(bar, r);
+                    send<V>(to, all.A, their);
+                    send<V>(to + 4 * V, all.H, their);
                 }
             }
-            cluster_arrive();
-            cluster_wait();
+            // a set is written again two joinings on, by CTAs that have this CTA's map of the one between, which is sent
+            // when all of its threads have read this one
+            const bool ok = mbar_wait(bar, (turn >> 1) & 1, &s.gave_up);
+            for (int r = 0; r < rank; ++r) apply<V>(s.cta[set][r][c], carry);
 #pragma unroll
             for (int v = 0; v < V; ++v) h[v] = carry[v];
-            for (int r = 0; r < csize; ++r) {
-                const Map<V> m2 = s.cta[parity][r][c];
+            for (int r = rank; r < csize; ++r) apply<V>(s.cta[set][r][c], carry);
+            if (!ok) {                  // a wait that gave up leaves NaN, not something that looks like a result
 #pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    if (r == rank) h[v] = carry[v];
-                    carry[v] = apply_map(m2.A[v], m2.H[v], carry[v]);
-                }
+                for (int v = 0; v < V; ++v) h[v] = carry[v] = __uint_as_float(0x7fffffffu);
             }
+            for (int w = 0; w < warp; ++w) apply<V>(s.warp[set][w][c], h);
         } else {
+            for (int w = 0; w < warp; ++w) apply<V>(s.warp[set][w][c], carry);
+#pragma unroll
+            for (int v = 0; v < V; ++v) h[v] = carry[v];
+            for (int w = warp; w < nwarps; ++w) apply<V>(s.warp[set][w][c], carry);
+        }
+        ++turn;
+        if (L::kSpans > 1) {
+            Map<V> e;
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                h[v] = carry[v];
-                carry[v] = apply_map(all.A[v], all.H[v], carry[v]);
+                e.A[v] = __shfl_up_sync(0xffffffffu, upto.A[v], L::kLanes % 32);
+                e.H[v] = __shfl_up_sync(0xffffffffu, upto.H[v], L::kLanes % 32);
             }
+            if (order > 0) apply<V>(e, h);
         }
 #pragma unroll
-        for (int v = 0; v < V; ++v) before[v] = apply_map(pre.A[v], pre.H[v], apply_map(front.A[v], front.H[v], h[v]));
+        for (int v = 0; v < V; ++v) before[v] = h[v];
     }
 };
 
-template <typename T, int V, int LX>
+// ---------------------------------------------------------------------------------------------------
+// A thread's inputs, kDepth spans ahead of their use: N matrices, kSteps vectors of each.  Vectors of 4 and 8 bytes are copied
+// asynchronously into the thread's own places in shared memory (nobody else touches them: no barrier); two bytes are the one size
+// that such a copy does not have, and wait in registers, one span ahead.
+// ---------------------------------------------------------------------------------------------------
+template <typename T, int V, int N>
+struct Ahead {
+    static constexpr int kSteps = Lay<V>::kSteps, kBytes = sizeof(T) * V, kDepth = 2;
+    static constexpr int kSmem = (kDepth + 1) * N * kSteps * kThreads * kBytes;
+    unsigned char *mine;
+    int put = 0, take = 0;
+    __device__ explicit Ahead(unsigned char *smem) : mine(smem + threadIdx.x * kBytes) {}
+    static __device__ __forceinline__ int place(int stage, int i, int k) { return ((stage * N + i) * kSteps + k) * kThreads * kBytes; }
+    // n steps of N matrices, from p[i] on, step[i] elements apart
+    __device__ __forceinline__ void fetch(const T *const (&p)[N], const long long (&step)[N], int n)
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const uint32_t to = smem_u32(mine + place(put, i, 0));
+            const T *q = p[i];
+            if (n == kSteps) {
+#pragma unroll
+                for (int k = 0; k < kSteps; ++k) {
+                    asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to + k * kThreads * kBytes), "l"(q), "n"(kBytes) : "memory");
+                    q += step[i];
+                }
+            } else {
+                for (int k = 0; k < n; ++k) {
+                    asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to + k * kThreads * kBytes), "l"(q), "n"(kBytes) : "memory");
+                    q += step[i];
+                }
+            }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        put = put == kDepth ? 0 : put + 1;
+    }
+    __device__ __forceinline__ void arrived() { asm volatile("cp.async.wait_group %0;" ::"n"(kDepth) : "memory"); }
+    __device__ __forceinline__ Vec<T, V> get_vec(int i, int k) const { return *reinterpret_cast<const Vec<T, V> *>(mine + place(take, i, k)); }
+    __device__ __forceinline__ void next_if_registers() {}
+    __device__ __forceinline__ void next() { take = take == kDepth ? 0 : take + 1; }
+};
+template <int N>
+struct Ahead<__nv_bfloat16, 1, N> {
+    typedef __nv_bfloat16 T;
+    static constexpr int kSteps = Lay<1>::kSteps, kDepth = 1, kSmem = 0;
+    Vec<T, 1> held[2][N][kSteps];
+    __device__ explicit Ahead(unsigned char *) {}
+    __device__ __forceinline__ void fetch(const T *const (&p)[N], const long long (&step)[N], int n)
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const T *q = p[i];
+#pragma unroll
+            for (int k = 0; k < kSteps; ++k) {
+                if (k < n) held[1][i][k] = load_vec<T, 1>(q);
+                q += step[i];
+            }
+        }
+    }
+    __device__ __forceinline__ void arrived() {}
+    __device__ __forceinline__ Vec<T, 1> get_vec(int i, int k) const { return held[0][i][k]; }
+    __device__ __forceinline__ void next() {}
+    __device__ __forceinline__ void next_if_registers()
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+            for (int k = 0; k < kSteps; ++k) held[0][i][k] = held[1][i][k];
+    }
+};
+
+// What a thread works on
+template <int V>
+struct Place {
+    int b, d, len, end;         // steps of the sequence; of the batch (0 where there is no such channel)
+    long long bd, BD;
+    bool live;
+    __device__ explicit Place(const LinrecArgs &p)
+    {
+        const long long vec = (long long)(blockIdx.x / p.csize) * Lay<V>::kLanes + threadIdx.x % Lay<V>::kLanes;
+        live = vec < (long long)p.B * p.nvec;
+        b = live ? (int)(vec / p.nvec) : 0;
+        d = live ? (int)(vec % p.nvec) * V : 0;
+        len = !live ? 0 : p.lengths ? min(max(p.lengths[b], 0), p.T) : p.T;
+        end = live ? p.T : 0;
+        bd = (long long)b * p.D + d;
+        BD = (long long)p.B * p.D;
+    }
+    // steps of the span from i0 that lie in front of `last`
+    static __device__ __forceinline__ int count(long long i0, int last)
+    {
+        return i0 < 0 ? 0 : (int)min((long long)Lay<V>::kSteps, max(0ll, last - i0));
+    }
+};
+
+template <typename T, int V, bool GATE>
 __global__ void __launch_bounds__(kThreads, 4) linrec_forward_kernel(const __grid_constant__ LinrecArgs p)
 {
-    using J = Joiner<V, LX>;
-    __shared__ typename J::Shared sh;
-    const int rank = p.csize > 1 ? (int)cluster_rank() : 0;
-    if (p.csize > 1) cluster_arrive();                  // the others' shared memory may be written once they have started
-    const int c = threadIdx.x % LX, seg = threadIdx.x / LX, segs = blockDim.x / LX;
-    const long long vec = (long long)(blockIdx.x / p.csize) * LX + c;
-    const bool live = vec < (long long)p.B * p.nvec;
-    const int b = live ? (int)(vec / p.nvec) : 0, d = live ? (int)(vec % p.nvec) * V : 0;
-    int len = !live ? 0 : p.lengths ? min(max(p.lengths[b], 0), p.T) : p.T;
-    const int end = live ? p.T : 0;
-    const long long bd = (long long)b * p.D + d, BD = (long long)p.B * p.D;
+    typedef Lay<V> L;
+    constexpr int kSteps = L::kSteps;
+    extern __shared__ __align__(16) unsigned char smem[];
+    __shared__ typename Joiner<V, GATE>::Shared sh;
+    Joiner<V, GATE> joiner(sh, p.csize);
+    const Place<V> at(p);
+    const long long sign = p.reverse ? -1 : 1;
+    const long long step[2] = {sign * p.a_t, sign * p.x_t}, out_step = sign * p.h_t;
+    T *ph = (T *)p.h + at.b * p.h_b + at.d;
+
+    const int span = blockDim.x / L::kLanes * p.csize * kSteps;
+    long long i0 = (long long)(joiner.rank * (blockDim.x / L::kLanes) + threadIdx.x / L::kLanes) * kSteps;
+    Ahead<T, V, 2> in(smem);
+    const T *from[2];
+    {
+        const long long t0 = p.reverse ? at.len - 1 - i0 : i0;
+        from[0] = (const T *)p.a + at.b * p.a_b + at.d + t0 * p.a_t;
+        from[1] = (const T *)p.x + at.b * p.x_b + at.d + t0 * p.x_t;
+    }
+    long long ahead = i0;
+    auto fetch = [&]() {
+        in.fetch(from, step, Place<V>::count(ahead, at.len));
+        ahead += span;
+        from[0] += span * step[0];
+        from[1] += span * step[1];
+    };
+#pragma unroll
+    for (int i = 0; i < Ahead<T, V, 2>::kDepth; ++i) fetch();
     float carry[V];
 #pragma unroll
-    for (int v = 0; v < V; ++v) carry[v] = live && p.h0 ? p.h0[bd + v] : 0.0f;
-    const long long back = p.reverse ? -1 : 1;
-    if (p.csize > 1) cluster_wait();
-
-    const int span = kSeg * segs * p.csize;
-    int parity = 0;
-    for (long long base = 0; base < p.T; base += span, parity ^= 1) {
-        const long long i0 = base + (long long)(rank * segs + seg) * kSeg;
-        const long long t0 = p.reverse ? len - 1 - i0 : i0;
-        const T *pa = (const T *)p.a + t0 * p.a_t + b * p.a_b + d, *px = (const T *)p.x + t0 * p.x_t + b * p.x_b + d;
-        const long long sa = back * p.a_t, sx = back * p.x_t;
-        const int n = (int)min((long long)kSeg, max(0ll, len - i0));
-        float f[kSeg][V], add[kSeg][V];
-        Vec<T, V> ra[kSeg], rx[kSeg];
+    for (int v = 0; v < V; ++v) carry[v] = at.live && p.h0 ? p.h0[at.bd + v] : 0.0f;
+    joiner.ready();
+    for (long long base = 0; base < p.T; base += span, i0 += span) {
+        const int n = Place<V>::count(i0, at.len);
+        in.next_if_registers();
+        fetch();
+        in.arrived();
+        float f[kSteps][V], add[kSteps][V];
 #pragma unroll
-        for (int k = 0; k < kSeg; ++k) {
-            if (k < n) {
-                ra[k] = load_vec<T, V>(pa + k * sa);
-                rx[k] = load_vec<T, V>(px + k * sx);
-            } else {
-                ra[k] = rx[k] = zero_vec<T, V>();
+        for (int k = 0; k < kSteps; ++k) {
+            const Vec<T, V> ra = in.get_vec(0, k), rx = in.get_vec(1, k);
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                f[k][v] = get<T, V>(ra, v);
+                add[k][v] = get<T, V>(rx, v);
+                if (GATE) {
+                    float w;
+                    gate_pair<T>(f[k][v], f[k][v], w);
+                    add[k][v] *= w;
+                }
+            }
+        }
+        in.next();
+        if (n < kSteps) {               // steps behind the end keep the state
+#pragma unroll
+            for (int k = 0; k < kSteps; ++k) {
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    f[k][v] = k < n ? f[k][v] : 1.0f;
+                    add[k][v] = k < n ? add[k][v] : 0.0f;
+                }
             }
         }
         Map<V> m;
 #pragma unroll
-        for (int v = 0; v < V; ++v) { m.A[v] = 1.0f; m.H[v] = 0.0f; }
+        for (int v = 0; v < V; ++v) {
+            m.A[v] = f[0][v];
+            m.H[v] = add[0][v];
 #pragma unroll
-        for (int k = 0; k < kSeg; ++k) {
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const float av = get<T, V>(ra[k], v), xv = get<T, V>(rx[k], v);
-                float fv = av, bv = xv;
-                if (p.gate) {
-                    float w;
-                    gate_pair<T>(av, fv, w);
-                    bv = w * xv;
-                }
-                f[k][v] = k < n ? fv : 1.0f;
-                add[k][v] = k < n ? bv : 0.0f;
+            for (int k = 1; k < kSteps; ++k) {
                 m.H[v] = fmaf(f[k][v], m.H[v], add[k][v]);
                 m.A[v] *= f[k][v];
             }
+            m.A[v] = held<V, GATE>(m.A[v]);
         }
         float h[V];
-        J::join(sh, parity, m, p.csize, rank, carry, h);
-        if (p.states && i0 < end) store_vec<float, V>(p.states + (i0 / kSeg) * BD + bd, h);
-        const int rows = (int)min((long long)kSeg, max(0ll, end - i0));
-        T *ph = (T *)p.h + b * p.h_b + d;
+        joiner.join(m, carry, h);
+        if (p.states && i0 < at.end && i0 % LSTM_LINREC_SEGMENT == 0)
+            store_vec<float, V>(p.states + i0 / LSTM_LINREC_SEGMENT * at.BD + at.bd, h);
+        const long long t0 = p.reverse ? at.len - 1 - i0 : i0;
+        if (n == kSteps) {
+            T *q = ph + t0 * p.h_t;
 #pragma unroll
-        for (int k = 0; k < kSeg; ++k) {
-            float o[V];
+            for (int k = 0; k < kSteps; ++k) {
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                h[v] = fmaf(f[k][v], h[v], add[k][v]);
-                o[v] = k < n ? h[v] : 0.0f;
+                for (int v = 0; v < V; ++v) h[v] = fmaf(f[k][v], h[v], add[k][v]);
+                store_vec<T, V>(q, h);
+                q += out_step;
             }
-            // steps behind a sequence's end lie at their own place in either direction
-            if (k < rows) store_vec<T, V>(ph + (k < n ? t0 + back * k : i0 + k) * p.h_t, o);
+        } else {
+            const int rows = Place<V>::count(i0, at.end);
+#pragma unroll
+            for (int k = 0; k < kSteps; ++k) {
+                float o[V];
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    h[v] = fmaf(f[k][v], h[v], add[k][v]);
+                    o[v] = k < n ? h[v] : 0.0f;
+                }
+                // steps behind a sequence's end lie at their own place in either direction
+                if (k < rows) store_vec<T, V>(ph + (k < n ? (p.reverse ? t0 - k : t0 + k) : i0 + k) * p.h_t, o);
+            }
         }
     }
-    if (p.hT && live && rank == 0 && seg == 0) store_vec<float, V>(p.hT + bd, carry);
+    if (p.hT && at.live && joiner.rank == 0 && threadIdx.x < L::kLanes) store_vec<float, V>(p.hT + at.bd, carry);
+    joiner.leave();
 }
 
-template <typename T, int V, int LX>
-__global__ void __launch_bounds__(kThreads, 3) linrec_backward_kernel(const __grid_constant__ LinrecArgs p)
+template <typename T, int V, bool GATE>
+__global__ void __launch_bounds__(kThreads, V == 4 ? 2 : 3) linrec_backward_kernel(const __grid_constant__ LinrecArgs p)
 {
-    using J = Joiner<V, LX>;
-    __shared__ typename J::Shared sh;
-    const int rank = p.csize > 1 ? (int)cluster_rank() : 0;
-    if (p.csize > 1) cluster_arrive();
-    const int c = threadIdx.x % LX, seg = threadIdx.x / LX, segs = blockDim.x / LX;
-    const long long vec = (long long)(blockIdx.x / p.csize) * LX + c;
-    const bool live = vec < (long long)p.B * p.nvec;
-    const int b = live ? (int)(vec / p.nvec) : 0, d = live ? (int)(vec % p.nvec) * V : 0;
-    const int len = !live ? 0 : p.lengths ? min(max(p.lengths[b], 0), p.T) : p.T;
-    const int end = live ? p.T : 0;
-    const long long bd = (long long)b * p.D + d, BD = (long long)p.B * p.D;
-    float carry[V];                                     // what reaches the state behind the steps that are left
-#pragma unroll
-    for (int v = 0; v < V; ++v) carry[v] = live && p.h0 ? p.h0[bd + v] : 0.0f;
-    const long long back = p.reverse ? -1 : 1;
-    if (p.csize > 1) cluster_wait();
+    typedef Lay<V> L;
+    constexpr int kSteps = L::kSteps;
+    extern __shared__ __align__(16) unsigned char smem[];
+    __shared__ typename Joiner<V, GATE>::Shared sh;
+    Joiner<V, GATE> joiner(sh, p.csize);
+    const Place<V> at(p);
+    const long long sign = p.reverse ? -1 : 1;
+    const long long step[3] = {sign * p.a_t, sign * p.x_t, sign * p.dh_t};
+    T *pda = (T *)p.da + at.b * p.da_b + at.d, *pdx = (T *)p.h + at.b * p.h_b + at.d;
 
-    const long long nseg = (p.T + kSeg - 1) / kSeg;
-    const int span = segs * p.csize;
-    int parity = 0;
-    for (long long base = 0; base < nseg; base += span, parity ^= 1) {
-        const long long sg = nseg - 1 - (base + rank * segs + seg);
-        const long long i0 = sg * kSeg;
-        const long long t0 = p.reverse ? len - 1 - i0 : i0;
-        const int n = sg < 0 ? 0 : (int)min((long long)kSeg, max(0ll, len - i0));
-        const T *pa = (const T *)p.a + t0 * p.a_t + b * p.a_b + d, *px = (const T *)p.x + t0 * p.x_t + b * p.x_b + d;
-        const T *pd = (const T *)p.dh + t0 * p.dh_t + b * p.dh_b + d;
-        const long long sa = back * p.a_t, sx = back * p.x_t, sd = back * p.dh_t;
-        Vec<T, V> ra[kSeg], rx[kSeg], rd[kSeg];
-        float h[V];
+    // Spans are joined from the last to the first: the first in the joining are the latest in the order of processing.
+    const long long nspan = ((long long)p.T + L::kWarpSteps - 1) / L::kWarpSteps * L::kSpans;
+    const int span = blockDim.x / L::kLanes * p.csize * kSteps;
+    long long i0 = (nspan - 1 - (long long)(joiner.rank * (blockDim.x / L::kLanes) + threadIdx.x / L::kLanes)) * kSteps;
+    const bool begins = i0 % LSTM_LINREC_SEGMENT == 0;      // a saved state stands in front of the thread's steps
+    Ahead<T, V, 3> in(smem);
+    const T *from[3];
+    {
+        const long long t0 = p.reverse ? at.len - 1 - i0 : i0;
+        from[0] = (const T *)p.a + at.b * p.a_b + at.d + t0 * p.a_t;
+        from[1] = (const T *)p.x + at.b * p.x_b + at.d + t0 * p.x_t;
+        from[2] = (const T *)p.dh + at.b * p.dh_b + at.d + t0 * p.dh_t;
+    }
+    long long ahead = i0;
+    auto fetch = [&]() {
+        in.fetch(from, step, Place<V>::count(ahead, at.len));
+        ahead -= span;
 #pragma unroll
-        for (int v = 0; v < V; ++v) h[v] = 0.0f;
-        if (n > 0) {
+        for (int i = 0; i < 3; ++i) from[i] -= span * step[i];
+    };
+    auto saved = [&](long long i, float (&h)[V]) {
+        const bool here = begins && i >= 0 && i < at.len;
 #pragma unroll
-            for (int v = 0; v < V; ++v) h[v] = p.states[sg * BD + bd + v];
-        }
+        for (int v = 0; v < V; ++v) h[v] = here ? p.states[i / LSTM_LINREC_SEGMENT * at.BD + at.bd + v] : 0.0f;
+    };
 #pragma unroll
-        for (int k = 0; k < kSeg; ++k) {
-            if (k < n) {
-                ra[k] = load_vec<T, V>(pa + k * sa);
-                rx[k] = load_vec<T, V>(px + k * sx);
-                rd[k] = load_vec<T, V>(pd + k * sd);
-            } else {
-                ra[k] = rx[k] = rd[k] = zero_vec<T, V>();
-            }
-        }
+    for (int i = 0; i < Ahead<T, V, 3>::kDepth; ++i) fetch();
+    float carry[V], hs[V];                              // carry: what reaches the state behind the steps that are left
+#pragma unroll
+    for (int v = 0; v < V; ++v) carry[v] = at.live && p.h0 ? p.h0[at.bd + v] : 0.0f;
+    saved(i0, hs);
+    joiner.ready();
+    for (long long base = 0; base < nspan * kSteps; base += span, i0 -= span) {
+        const int n = Place<V>::count(i0, at.len);
+        in.next_if_registers();
+        fetch();
+        in.arrived();
         // da_t = g_t u_t and dx_t = g_t w_t with u = (h_{t-1} - x) f (1 - f), w = 1 - f  (decay: u = h_{t-1}, w = 1)
-        float f[kSeg][V], u[kSeg][V], w[kSeg][V];
+        float f[kSteps][V], u[kSteps][V], w[kSteps][V], d[kSteps][V];
 #pragma unroll
-        for (int k = 0; k < kSeg; ++k) {
+        for (int k = 0; k < kSteps; ++k) {
+            const Vec<T, V> ra = in.get_vec(0, k), rx = in.get_vec(1, k), rd = in.get_vec(2, k);
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const float av = get<T, V>(ra[k], v), xv = get<T, V>(rx[k], v);
-                float fv = av, wv = 1.0f, uv = h[v], bv = xv;
-                if (p.gate) {
-                    gate_pair<T>(av, fv, wv);
-                    uv = (h[v] - xv) * (fv * wv);
-                    bv = wv * xv;
-                }
-                h[v] = fmaf(fv, h[v], bv);
-                f[k][v] = k < n ? fv : 1.0f;
-                u[k][v] = uv;
-                w[k][v] = wv;
+                f[k][v] = get<T, V>(ra, v);
+                u[k][v] = get<T, V>(rx, v);
+                d[k][v] = get<T, V>(rd, v);
+                w[k][v] = 1.0f;
+                if (GATE) gate_pair<T>(f[k][v], f[k][v], w[k][v]);
             }
+        }
+        in.next();
+        float h[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) h[v] = hs[v];
+        if (V > 1) {
+            // the state behind the first 8 of a segment's steps is the one in front of its other 8, which the lanes below hold
+#pragma unroll
+            for (int k = 0; k < kSteps; ++k)
+#pragma unroll
+                for (int v = 0; v < V; ++v) h[v] = fmaf(f[k][v], h[v], w[k][v] * u[k][v]);
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const float behind = __shfl_down_sync(0xffffffffu, h[v], L::kLanes % 32);
+                h[v] = begins ? hs[v] : behind;
+            }
+        }
+        saved(i0 - span, hs);
+#pragma unroll
+        for (int k = 0; k < kSteps; ++k) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const float x = u[k][v], before = h[v];
+                h[v] = fmaf(f[k][v], before, w[k][v] * x);
+                u[k][v] = GATE ? (before - x) * (f[k][v] * w[k][v]) : before;
+            }
+        }
+        if (n < kSteps) {
+#pragma unroll
+            for (int k = 0; k < kSteps; ++k)
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    f[k][v] = k < n ? f[k][v] : 1.0f;
+                    d[k][v] = k < n ? d[k][v] : 0.0f;
+                }
         }
         Map<V> m;
 #pragma unroll
-        for (int v = 0; v < V; ++v) { m.A[v] = 1.0f; m.H[v] = 0.0f; }
+        for (int v = 0; v < V; ++v) {
+            m.A[v] = f[kSteps - 1][v];
+            m.H[v] = f[kSteps - 1][v] * d[kSteps - 1][v];
 #pragma unroll
-        for (int k = kSeg - 1; k >= 0; --k) {
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                m.H[v] = f[k][v] * (get<T, V>(rd[k], v) + m.H[v]);
+            for (int k = kSteps - 2; k >= 0; --k) {
+                m.H[v] = f[k][v] * (d[k][v] + m.H[v]);
                 m.A[v] *= f[k][v];
             }
+            m.A[v] = held<V, GATE>(m.A[v]);
         }
         float q[V];
-        J::join(sh, parity, m, p.csize, rank, carry, q);
-        const int rows = sg < 0 ? 0 : (int)min((long long)kSeg, max(0ll, end - i0));
-        T *pda = (T *)p.da + b * p.da_b + d, *pdx = (T *)p.h + b * p.h_b + d;
+        joiner.join(m, carry, q);
+        const long long t0 = p.reverse ? at.len - 1 - i0 : i0;
+        if (n == kSteps) {
+            const long long last = p.reverse ? t0 - (kSteps - 1) : t0 + kSteps - 1;
+            T *qa = pda + last * p.da_t, *qx = pdx + last * p.h_t;
 #pragma unroll
-        for (int k = kSeg - 1; k >= 0; --k) {
-            float oa[V], ox[V];
+            for (int k = kSteps - 1; k >= 0; --k) {
+                float oa[V], ox[V];
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const float g = get<T, V>(rd[k], v) + q[v];
-                oa[v] = k < n ? g * u[k][v] : 0.0f;
-                ox[v] = k < n ? g * w[k][v] : 0.0f;
-                q[v] = f[k][v] * g;
+                for (int v = 0; v < V; ++v) {
+                    const float g = d[k][v] + q[v];
+                    oa[v] = g * u[k][v];
+                    ox[v] = g * w[k][v];
+                    q[v] = f[k][v] * g;
+                }
+                store_vec<T, V>(qa, oa);
+                store_vec<T, V>(qx, ox);
+                qa -= sign * p.da_t;
+                qx -= sign * p.h_t;
             }
-            if (k < rows) {
-                const long long t = k < n ? t0 + back * k : i0 + k;
-                store_vec<T, V>(pda + t * p.da_t, oa);
-                store_vec<T, V>(pdx + t * p.h_t, ox);
+        } else {
+            const int rows = Place<V>::count(i0, at.end);
+#pragma unroll
+            for (int k = kSteps - 1; k >= 0; --k) {
+                float oa[V], ox[V];
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    const float g = d[k][v] + q[v];
+                    oa[v] = k < n ? g * u[k][v] : 0.0f;
+                    ox[v] = k < n ? g * w[k][v] : 0.0f;
+                    q[v] = f[k][v] * g;
+                }
+                if (k < rows) {
+                    const long long t = k < n ? (p.reverse ? t0 - k : t0 + k) : i0 + k;
+                    store_vec<T, V>(pda + t * p.da_t, oa);
+                    store_vec<T, V>(pdx + t * p.h_t, ox);
+                }
             }
         }
     }
-    if (p.hT && live && rank == 0 && seg == 0) store_vec<float, V>(p.hT + bd, carry);
+    if (p.hT && at.live && joiner.rank == 0 && threadIdx.x < L::kLanes) store_vec<float, V>(p.hT + at.bd, carry);
+    joiner.leave();
 }
 
-template <typename T, int V, int LX>
+template <typename T, int V, bool GATE>
 cudaError_t launch(LinrecArgs &p, bool backward, int sms, cudaStream_t st)
 {
-    const void *fn = backward ? (const void *)linrec_backward_kernel<T, V, LX> : (const void *)linrec_forward_kernel<T, V, LX>;
-    const long long groups = ((long long)p.B * p.nvec + LX - 1) / LX, need = ((long long)p.T + kSeg - 1) / kSeg;
-    // segments of a CTA: whole warps, no more than there are steps for
-    int segs = kThreads / LX;
-    while (segs > 32 / LX && segs / 2 >= need) segs /= 2;
-    // CTAs of a cluster: as many as leave no SM short of work, no more than there are steps for
+    typedef Lay<V> L;
+    const void *fn = backward ? (const void *)linrec_backward_kernel<T, V, GATE> : (const void *)linrec_forward_kernel<T, V, GATE>;
+    const long long groups = ((long long)p.B * p.nvec + L::kLanes - 1) / L::kLanes, need = ((long long)p.T + L::kWarpSteps - 1) / L::kWarpSteps;
+    // warps of a CTA: no more than there are steps for
+    const int warps = need >= kThreads / 32 ? kThreads / 32 : need > 1 ? (int)need : 1;
+    // CTAs of a cluster: as many as leave no SM short of work, no more than there are steps for; 16 (which few places on
+    // the chip can hold) only where 8 do not reach every SM
     int csize = 1;
-    while (csize < 16 && groups * csize < 4ll * sms && (long long)segs * csize < need) csize *= 2;
+    while (csize < kMaxCluster && groups * csize < (csize < 8 ? 3ll : 1ll) * sms && (long long)warps * csize < need) csize *= 2;
     p.csize = csize;
     if (groups * csize > 0x7fffffffll) return cudaErrorInvalidConfiguration;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(groups * csize));
-    cfg.blockDim = dim3((unsigned)(segs * LX));
+    cfg.blockDim = dim3((unsigned)(warps * 32));
+    cfg.dynamicSmemBytes = backward ? Ahead<T, V, 3>::kSmem : Ahead<T, V, 2>::kSmem;
     cfg.stream = st;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension;
@@ -370,32 +610,39 @@ cudaError_t launch(LinrecArgs &p, bool backward, int sms, cudaStream_t st)
     at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = csize > 1 ? 1 : 0;
-    if (csize > 8) {
-        const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-        if (e != cudaSuccess) return e;
-    }
+    cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg.dynamicSmemBytes);
+    if (e == cudaSuccess && csize > 8) e = cudaFuncSetAttribute(fn, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e != cudaSuccess) return e;
     void *args[] = {&p};
     return cudaLaunchKernelExC(&cfg, fn, args);
 }
 
 template <typename T, int V>
-cudaError_t by_lanes(LinrecArgs &p, bool backward, int sms, cudaStream_t st)
+cudaError_t by_gate(LinrecArgs &p, bool backward, int sms, cudaStream_t st)
 {
-    // 32 vectors side by side where there are channels enough for all SMs with clusters of 16, else 16 and two segments a warp
-    const long long vecs = (long long)p.B * p.nvec;
-    return vecs * 16 >= 32ll * 4 * sms || p.T <= 4 * kSeg ? launch<T, V, 32>(p, backward, sms, st) : launch<T, V, 16>(p, backward, sms, st);
+    p.nvec = p.D / V;
+    return p.gate ? launch<T, V, true>(p, backward, sms, st) : launch<T, V, false>(p, backward, sms, st);
 }
 
+// the widest vector, of up to 8 bytes, that divides the channels and to which every matrix is aligned
 template <typename T>
 cudaError_t by_vector(LinrecArgs &p, bool backward, int sms, cudaStream_t st)
 {
-    const size_t es = sizeof(T);
-    auto even = [&](const void *q, long long t, long long b) { return (uintptr_t)q % (2 * es) == 0 && t % 2 == 0 && b % 2 == 0; };
-    auto even_f = [](const void *q) { return (uintptr_t)q % 8 == 0; };
-    bool two = p.D % 2 == 0 && even(p.a, p.a_t, p.a_b) && even(p.x, p.x_t, p.x_b) && even(p.h, p.h_t, p.h_b) && even_f(p.hT) && even_f(p.states);
-    if (backward) two = two && even(p.dh, p.dh_t, p.dh_b) && even(p.da, p.da_t, p.da_b);
-    p.nvec = two ? p.D / 2 : p.D;
-    return two ? by_lanes<T, 2>(p, backward, sms, st) : by_lanes<T, 1>(p, backward, sms, st);
+    constexpr int kMost = 8 / sizeof(T);
+    int v = kMost;
+    while (p.D % v) v /= 2;
+    auto matrix = [&](const void *q, long long t, long long b, int es) {
+        while (v > 1 && q && ((uintptr_t)q % (v * es) || t % v || b % v)) v /= 2;
+    };
+    matrix(p.a, p.a_t, p.a_b, sizeof(T));
+    matrix(p.x, p.x_t, p.x_b, sizeof(T));
+    matrix(p.h, p.h_t, p.h_b, sizeof(T));
+    matrix(p.dh, p.dh_t, p.dh_b, sizeof(T));
+    matrix(p.da, p.da_t, p.da_b, sizeof(T));
+    matrix(p.hT, 0, 0, 4);
+    matrix(p.states, 0, 0, 4);
+    if (v == kMost) return by_gate<T, kMost>(p, backward, sms, st);
+    return v == 2 ? by_gate<T, 2>(p, backward, sms, st) : by_gate<T, 1>(p, backward, sms, st);
 }
 
 int run(LinrecArgs &p, int dtype, bool backward, cudaStream_t st, const Failure &fail)
