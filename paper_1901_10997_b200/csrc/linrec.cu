@@ -62,23 +62,73 @@ __device__ __forceinline__ float rcp_fast(float x)
 
 // f and 1 - f, both to full relative accuracy: with e = exp(-|u|) they are 1/(1+e) and e/(1+e), in the order that the sign says.
 // bf16 data: the hardware's exponential (error 2^-22 and |u| 2^-24) is far inside a rounding to 8 bits; fp32 data: expf.
-template <typename T>
-__device__ __forceinline__ void gate_pair(float u, float &f, float &w)
+// d = a b + c and d = a b over the channels of a vector, two to an instruction
+template <int V>
+__device__ __forceinline__ void fma_vec(float (&d)[V], const float (&a)[V], const float (&b)[V], const float (&c)[V])
 {
-    const float e = sizeof(T) == 2 ? ex2_fast(-1.4426950408889634f * fabsf(u)) : expf(-fabsf(u));
-    const float s = rcp_fast(1.0f + e), r = e * s;
-    f = u >= 0.0f ? s : r;
-    w = u >= 0.0f ? r : s;
+    if (V == 1) { d[0] = fmaf(a[0], b[0], c[0]); return; }
+#pragma unroll
+    for (int v = 0; v + 1 < V; v += 2)
+        asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\t"
+            "fma.rn.f32x2 x, x, y, z;\n\tmov.b64 {%0, %1}, x;\n\t}"
+            : "=f"(d[v]), "=f"(d[v + 1]) : "f"(a[v]), "f"(a[v + 1]), "f"(b[v]), "f"(b[v + 1]), "f"(c[v]), "f"(c[v + 1]));
+}
+template <int V>
+__device__ __forceinline__ void mul_vec(float (&d)[V], const float (&a)[V], const float (&b)[V])
+{
+    if (V == 1) { d[0] = a[0] * b[0]; return; }
+#pragma unroll
+    for (int v = 0; v + 1 < V; v += 2)
+        asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmul.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
+            : "=f"(d[v]), "=f"(d[v + 1]) : "f"(a[v]), "f"(a[v + 1]), "f"(b[v]), "f"(b[v + 1]));
+}
+template <int V>
+__device__ __forceinline__ void add_vec(float (&d)[V], const float (&a)[V], const float (&b)[V])
+{
+    if (V == 1) { d[0] = a[0] + b[0]; return; }
+#pragma unroll
+    for (int v = 0; v + 1 < V; v += 2)
+        asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tadd.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
+            : "=f"(d[v]), "=f"(d[v + 1]) : "f"(a[v]), "f"(a[v + 1]), "f"(b[v]), "f"(b[v + 1]));
+}
+
+// u -> f and w = 1 - f
+template <typename T, int V>
+__device__ __forceinline__ void gate_vec(const float (&u)[V], float (&f)[V], float (&w)[V])
+{
+    float e[V], s[V], r[V], one[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        e[v] = sizeof(T) == 2 ? ex2_fast(-1.4426950408889634f * fabsf(u[v])) : expf(-fabsf(u[v]));
+        one[v] = 1.0f;
+    }
+    add_vec<V>(s, e, one);
+#pragma unroll
+    for (int v = 0; v < V; ++v) s[v] = rcp_fast(s[v]);
+    mul_vec<V>(r, e, s);
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        const bool open = u[v] >= 0.0f;
+        f[v] = open ? s[v] : r[v];
+        w[v] = open ? r[v] : s[v];
+    }
 }
 
 template <int V>
 struct alignas(8 * V) Map { float A[V], H[V]; };
 
 template <int V>
+__device__ __forceinline__ Map<V> identity()
+{
+    Map<V> m;
+#pragma unroll
+    for (int v = 0; v < V; ++v) { m.A[v] = 1.0f; m.H[v] = 0.0f; }
+    return m;
+}
+template <int V>
 __device__ __forceinline__ void apply(const Map<V> &m, float (&h)[V])
 {
-#pragma unroll
-    for (int v = 0; v < V; ++v) h[v] = fmaf(m.A[v], h[v], m.H[v]);
+    fma_vec<V>(h, m.A, h, m.H);
 }
 // m := later o m.  A product of decays that grew out of range is held at its edge: a state of zero stays zero behind it.
 template <int V, bool GATE>
@@ -223,12 +273,22 @@ struct Joiner {
     }
 };
 
+// what stands in the place of a step's logit or decay to keep the state
+template <typename T, int V, bool GATE>
+__device__ __forceinline__ Vec<T, V> keep()
+{
+    Vec<T, V> r;
+#pragma unroll
+    for (int v = 0; v < V; ++v) r.e[v] = T(GATE ? __int_as_float(0x7f800000) : 1.0f);
+    return r;
+}
+
 // ---------------------------------------------------------------------------------------------------
 // A thread's inputs, kDepth spans ahead of their use: N matrices, kSteps vectors of each.  Vectors of 4 and 8 bytes are copied
 // asynchronously into the thread's own places in shared memory (nobody else touches them: no barrier); two bytes are the one size
 // that such a copy does not have, and wait in registers, one span ahead.
 // ---------------------------------------------------------------------------------------------------
-template <typename T, int V, int N>
+template <typename T, int V, int N, bool GATE>
 struct Ahead {
     static constexpr int kSteps = Lay<V>::kSteps, kBytes = sizeof(T) * V, kDepth = 2;
     static constexpr int kSmem = (kDepth + 1) * N * kSteps * kThreads * kBytes;
@@ -249,9 +309,10 @@ struct Ahead {
                     asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to + k * kThreads * kBytes), "l"(q), "n"(kBytes) : "memory");
                     q += step[i];
                 }
-            } else {
-                for (int k = 0; k < n; ++k) {
-                    asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to + k * kThreads * kBytes), "l"(q), "n"(kBytes) : "memory");
+            } else {                    // steps behind the end keep the state
+                for (int k = 0; k < kSteps; ++k) {
+                    if (k < n) asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to + k * kThreads * kBytes), "l"(q), "n"(kBytes) : "memory");
+                    else *reinterpret_cast<Vec<T, V> *>(mine + place(put, i, k)) = i == 0 ? keep<T, V, GATE>() : zero_vec<T, V>();
                     q += step[i];
                 }
             }
@@ -264,8 +325,8 @@ struct Ahead {
     __device__ __forceinline__ void next_if_registers() {}
     __device__ __forceinline__ void next() { take = take == kDepth ? 0 : take + 1; }
 };
-template <int N>
-struct Ahead<__nv_bfloat16, 1, N> {
+template <int N, bool GATE>
+struct Ahead<__nv_bfloat16, 1, N, GATE> {
     typedef __nv_bfloat16 T;
     static constexpr int kSteps = Lay<1>::kSteps, kDepth = 1, kSmem = 0;
     Vec<T, 1> held[2][N][kSteps];
@@ -277,7 +338,7 @@ struct Ahead<__nv_bfloat16, 1, N> {
             const T *q = p[i];
 #pragma unroll
             for (int k = 0; k < kSteps; ++k) {
-                if (k < n) held[1][i][k] = load_vec<T, 1>(q);
+                held[1][i][k] = k < n ? load_vec<T, 1>(q) : i == 0 ? keep<T, 1, GATE>() : zero_vec<T, 1>();
                 q += step[i];
             }
         }
@@ -314,7 +375,7 @@ struct Place {
     // steps of the span from i0 that lie in front of `last`
     static __device__ __forceinline__ int count(long long i0, int last)
     {
-        return i0 < 0 ? 0 : (int)min((long long)Lay<V>::kSteps, max(0ll, last - i0));
+        return i0 < 0 || i0 >= last ? 0 : min(Lay<V>::kSteps, last - (int)i0);
     }
 };
 
@@ -333,22 +394,23 @@ __global__ void __launch_bounds__(kThreads, 4) linrec_forward_kernel(const __gri
 
     const int span = blockDim.x / L::kLanes * p.csize * kSteps;
     long long i0 = (long long)(joiner.rank * (blockDim.x / L::kLanes) + threadIdx.x / L::kLanes) * kSteps;
-    Ahead<T, V, 2> in(smem);
+    Ahead<T, V, 2, GATE> in(smem);
     const T *from[2];
     {
         const long long t0 = p.reverse ? at.len - 1 - i0 : i0;
         from[0] = (const T *)p.a + at.b * p.a_b + at.d + t0 * p.a_t;
         from[1] = (const T *)p.x + at.b * p.x_b + at.d + t0 * p.x_t;
     }
+    const long long jump[2] = {span * step[0], span * step[1]};
     long long ahead = i0;
     auto fetch = [&]() {
         in.fetch(from, step, Place<V>::count(ahead, at.len));
         ahead += span;
-        from[0] += span * step[0];
-        from[1] += span * step[1];
+        from[0] += jump[0];
+        from[1] += jump[1];
     };
 #pragma unroll
-    for (int i = 0; i < Ahead<T, V, 2>::kDepth; ++i) fetch();
+    for (int i = 0; i < Ahead<T, V, 2, GATE>::kDepth; ++i) fetch();
     float carry[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) carry[v] = at.live && p.h0 ? p.h0[at.bd + v] : 0.0f;
@@ -358,7 +420,10 @@ __global__ void __launch_bounds__(kThreads, 4) linrec_forward_kernel(const __gri
         in.next_if_registers();
         fetch();
         in.arrived();
+        const bool idle = __all_sync(0xffffffffu, n == 0);      // behind the end of all its sequences a warp only joins in
         float f[kSteps][V], add[kSteps][V];
+        Map<V> m = identity<V>();
+        if (!idle) {
 #pragma unroll
         for (int k = 0; k < kSteps; ++k) {
             const Vec<T, V> ra = in.get_vec(0, k), rx = in.get_vec(1, k);
@@ -366,36 +431,24 @@ __global__ void __launch_bounds__(kThreads, 4) linrec_forward_kernel(const __gri
             for (int v = 0; v < V; ++v) {
                 f[k][v] = get<T, V>(ra, v);
                 add[k][v] = get<T, V>(rx, v);
-                if (GATE) {
-                    float w;
-                    gate_pair<T>(f[k][v], f[k][v], w);
-                    add[k][v] *= w;
-                }
             }
+            if (GATE) {
+                float w[V];
+                gate_vec<T, V>(f[k], f[k], w);
+                mul_vec<V>(add[k], add[k], w);
+            }
+        }
+#pragma unroll
+        for (int v = 0; v < V; ++v) { m.A[v] = f[0][v]; m.H[v] = add[0][v]; }
+#pragma unroll
+        for (int k = 1; k < kSteps; ++k) {
+            fma_vec<V>(m.H, f[k], m.H, add[k]);
+            mul_vec<V>(m.A, m.A, f[k]);
+        }
+#pragma unroll
+        for (int v = 0; v < V; ++v) m.A[v] = held<V, GATE>(m.A[v]);
         }
         in.next();
-        if (n < kSteps) {               // steps behind the end keep the state
-#pragma unroll
-            for (int k = 0; k < kSteps; ++k) {
-#pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    f[k][v] = k < n ? f[k][v] : 1.0f;
-                    add[k][v] = k < n ? add[k][v] : 0.0f;
-                }
-            }
-        }
-        Map<V> m;
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            m.A[v] = f[0][v];
-            m.H[v] = add[0][v];
-#pragma unroll
-            for (int k = 1; k < kSteps; ++k) {
-                m.H[v] = fmaf(f[k][v], m.H[v], add[k][v]);
-                m.A[v] *= f[k][v];
-            }
-            m.A[v] = held<V, GATE>(m.A[v]);
-        }
         float h[V];
         joiner.join(m, carry, h);
         if (p.states && i0 < at.end && i0 % LSTM_LINREC_SEGMENT == 0)
@@ -405,21 +458,22 @@ __global__ void __launch_bounds__(kThreads, 4) linrec_forward_kernel(const __gri
             T *q = ph + t0 * p.h_t;
 #pragma unroll
             for (int k = 0; k < kSteps; ++k) {
-#pragma unroll
-                for (int v = 0; v < V; ++v) h[v] = fmaf(f[k][v], h[v], add[k][v]);
+                fma_vec<V>(h, f[k], h, add[k]);
                 store_vec<T, V>(q, h);
                 q += out_step;
             }
+        } else if (idle) {
+            const float zero[V] = {};
+            const int rows = Place<V>::count(i0, at.end);
+            for (int k = 0; k < rows; ++k) store_vec<T, V>(ph + (i0 + k) * p.h_t, zero);
         } else {
             const int rows = Place<V>::count(i0, at.end);
 #pragma unroll
             for (int k = 0; k < kSteps; ++k) {
                 float o[V];
+                fma_vec<V>(h, f[k], h, add[k]);
 #pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    h[v] = fmaf(f[k][v], h[v], add[k][v]);
-                    o[v] = k < n ? h[v] : 0.0f;
-                }
+                for (int v = 0; v < V; ++v) o[v] = k < n ? h[v] : 0.0f;
                 // steps behind a sequence's end lie at their own place in either direction
                 if (k < rows) store_vec<T, V>(ph + (k < n ? (p.reverse ? t0 - k : t0 + k) : i0 + k) * p.h_t, o);
             }
@@ -447,7 +501,7 @@ __global__ void __launch_bounds__(kThreads, V == 4 ? 2 : 3) linrec_backward_kern
     const int span = blockDim.x / L::kLanes * p.csize * kSteps;
     long long i0 = (nspan - 1 - (long long)(joiner.rank * (blockDim.x / L::kLanes) + threadIdx.x / L::kLanes)) * kSteps;
     const bool begins = i0 % LSTM_LINREC_SEGMENT == 0;      // a saved state stands in front of the thread's steps
-    Ahead<T, V, 3> in(smem);
+    Ahead<T, V, 3, GATE> in(smem);
     const T *from[3];
     {
         const long long t0 = p.reverse ? at.len - 1 - i0 : i0;
@@ -456,11 +510,12 @@ __global__ void __launch_bounds__(kThreads, V == 4 ? 2 : 3) linrec_backward_kern
         from[2] = (const T *)p.dh + at.b * p.dh_b + at.d + t0 * p.dh_t;
     }
     long long ahead = i0;
+    const long long jump[3] = {span * step[0], span * step[1], span * step[2]};
     auto fetch = [&]() {
         in.fetch(from, step, Place<V>::count(ahead, at.len));
         ahead -= span;
 #pragma unroll
-        for (int i = 0; i < 3; ++i) from[i] -= span * step[i];
+        for (int i = 0; i < 3; ++i) from[i] -= jump[i];
     };
     auto saved = [&](long long i, float (&h)[V]) {
         const bool here = begins && i >= 0 && i < at.len;
@@ -468,7 +523,7 @@ __global__ void __launch_bounds__(kThreads, V == 4 ? 2 : 3) linrec_backward_kern
         for (int v = 0; v < V; ++v) h[v] = here ? p.states[i / LSTM_LINREC_SEGMENT * at.BD + at.bd + v] : 0.0f;
     };
 #pragma unroll
-    for (int i = 0; i < Ahead<T, V, 3>::kDepth; ++i) fetch();
+    for (int i = 0; i < Ahead<T, V, 3, GATE>::kDepth; ++i) fetch();
     float carry[V], hs[V];                              // carry: what reaches the state behind the steps that are left
 #pragma unroll
     for (int v = 0; v < V; ++v) carry[v] = at.live && p.h0 ? p.h0[at.bd + v] : 0.0f;
@@ -480,7 +535,10 @@ __global__ void __launch_bounds__(kThreads, V == 4 ? 2 : 3) linrec_backward_kern
         fetch();
         in.arrived();
         // da_t = g_t u_t and dx_t = g_t w_t with u = (h_{t-1} - x) f (1 - f), w = 1 - f  (decay: u = h_{t-1}, w = 1)
+        const bool idle = __all_sync(0xffffffffu, n == 0);
         float f[kSteps][V], u[kSteps][V], w[kSteps][V], d[kSteps][V];
+        Map<V> m = identity<V>();
+        if (!idle) {
 #pragma unroll
         for (int k = 0; k < kSteps; ++k) {
             const Vec<T, V> ra = in.get_vec(0, k), rx = in.get_vec(1, k), rd = in.get_vec(2, k);
@@ -490,56 +548,58 @@ __global__ void __launch_bounds__(kThreads, V == 4 ? 2 : 3) linrec_backward_kern
                 u[k][v] = get<T, V>(rx, v);
                 d[k][v] = get<T, V>(rd, v);
                 w[k][v] = 1.0f;
-                if (GATE) gate_pair<T>(f[k][v], f[k][v], w[k][v]);
             }
+            if (GATE) gate_vec<T, V>(f[k], f[k], w[k]);
         }
-        in.next();
         float h[V];
 #pragma unroll
         for (int v = 0; v < V; ++v) h[v] = hs[v];
         if (V > 1) {
             // the state behind the first 8 of a segment's steps is the one in front of its other 8, which the lanes below hold
 #pragma unroll
-            for (int k = 0; k < kSteps; ++k)
-#pragma unroll
-                for (int v = 0; v < V; ++v) h[v] = fmaf(f[k][v], h[v], w[k][v] * u[k][v]);
+            for (int k = 0; k < kSteps; ++k) {
+                float b[V];
+                mul_vec<V>(b, w[k], u[k]);
+                fma_vec<V>(h, f[k], h, b);
+            }
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 const float behind = __shfl_down_sync(0xffffffffu, h[v], L::kLanes % 32);
                 h[v] = begins ? hs[v] : behind;
             }
         }
-        saved(i0 - span, hs);
 #pragma unroll
         for (int k = 0; k < kSteps; ++k) {
+            float b[V], fw[V], less[V];
+            if (GATE) {
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const float x = u[k][v], before = h[v];
-                h[v] = fmaf(f[k][v], before, w[k][v] * x);
-                u[k][v] = GATE ? (before - x) * (f[k][v] * w[k][v]) : before;
+                for (int v = 0; v < V; ++v) less[v] = h[v] - u[k][v];
+                mul_vec<V>(b, w[k], u[k]);
+                mul_vec<V>(fw, f[k], w[k]);
+                fma_vec<V>(h, f[k], h, b);
+                mul_vec<V>(u[k], less, fw);
+            } else {
+#pragma unroll
+                for (int v = 0; v < V; ++v) { less[v] = h[v]; b[v] = u[k][v]; }
+                fma_vec<V>(h, f[k], h, b);
+#pragma unroll
+                for (int v = 0; v < V; ++v) u[k][v] = less[v];
             }
         }
-        if (n < kSteps) {
 #pragma unroll
-            for (int k = 0; k < kSteps; ++k)
+        for (int v = 0; v < V; ++v) m.A[v] = f[kSteps - 1][v];
+        mul_vec<V>(m.H, f[kSteps - 1], d[kSteps - 1]);
 #pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    f[k][v] = k < n ? f[k][v] : 1.0f;
-                    d[k][v] = k < n ? d[k][v] : 0.0f;
-                }
+        for (int k = kSteps - 2; k >= 0; --k) {
+            add_vec<V>(m.H, m.H, d[k]);
+            mul_vec<V>(m.H, m.H, f[k]);
+            mul_vec<V>(m.A, m.A, f[k]);
         }
-        Map<V> m;
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            m.A[v] = f[kSteps - 1][v];
-            m.H[v] = f[kSteps - 1][v] * d[kSteps - 1][v];
-#pragma unroll
-            for (int k = kSteps - 2; k >= 0; --k) {
-                m.H[v] = f[k][v] * (d[k][v] + m.H[v]);
-                m.A[v] *= f[k][v];
-            }
-            m.A[v] = held<V, GATE>(m.A[v]);
+        for (int v = 0; v < V; ++v) m.A[v] = held<V, GATE>(m.A[v]);
         }
+        in.next();
+        saved(i0 - span, hs);
         float q[V];
         joiner.join(m, carry, q);
         const long long t0 = p.reverse ? at.len - 1 - i0 : i0;
@@ -548,18 +608,22 @@ __global__ void __launch_bounds__(kThreads, V == 4 ? 2 : 3) linrec_backward_kern
             T *qa = pda + last * p.da_t, *qx = pdx + last * p.h_t;
 #pragma unroll
             for (int k = kSteps - 1; k >= 0; --k) {
-                float oa[V], ox[V];
-#pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    const float g = d[k][v] + q[v];
-                    oa[v] = g * u[k][v];
-                    ox[v] = g * w[k][v];
-                    q[v] = f[k][v] * g;
-                }
+                float oa[V], ox[V], g[V];
+                add_vec<V>(g, d[k], q);
+                mul_vec<V>(oa, g, u[k]);
+                mul_vec<V>(ox, g, w[k]);
+                mul_vec<V>(q, g, f[k]);
                 store_vec<T, V>(qa, oa);
                 store_vec<T, V>(qx, ox);
                 qa -= sign * p.da_t;
                 qx -= sign * p.h_t;
+            }
+        } else if (idle) {
+            const float zero[V] = {};
+            const int rows = Place<V>::count(i0, at.end);
+            for (int k = 0; k < rows; ++k) {
+                store_vec<T, V>(pda + (i0 + k) * p.da_t, zero);
+                store_vec<T, V>(pdx + (i0 + k) * p.h_t, zero);
             }
         } else {
             const int rows = Place<V>::count(i0, at.end);
@@ -593,16 +657,16 @@ cudaError_t launch(LinrecArgs &p, bool backward, int sms, cudaStream_t st)
     const long long groups = ((long long)p.B * p.nvec + L::kLanes - 1) / L::kLanes, need = ((long long)p.T + L::kWarpSteps - 1) / L::kWarpSteps;
     // warps of a CTA: no more than there are steps for
     const int warps = need >= kThreads / 32 ? kThreads / 32 : need > 1 ? (int)need : 1;
-    // CTAs of a cluster: as many as leave no SM short of work, no more than there are steps for; 16 (which few places on
-    // the chip can hold) only where 8 do not reach every SM
+    // CTAs of a cluster: two for each SM, no more than there are steps for; 16 (which few places on the chip can hold) only
+    // where 8 do not reach every SM
     int csize = 1;
-    while (csize < kMaxCluster && groups * csize < (csize < 8 ? 3ll : 1ll) * sms && (long long)warps * csize < need) csize *= 2;
+    while (csize < kMaxCluster && groups * csize < (csize < 8 ? 2ll : 1ll) * sms && (long long)warps * csize < need) csize *= 2;
     p.csize = csize;
     if (groups * csize > 0x7fffffffll) return cudaErrorInvalidConfiguration;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(groups * csize));
     cfg.blockDim = dim3((unsigned)(warps * 32));
-    cfg.dynamicSmemBytes = backward ? Ahead<T, V, 3>::kSmem : Ahead<T, V, 2>::kSmem;
+    cfg.dynamicSmemBytes = backward ? Ahead<T, V, 3, GATE>::kSmem : Ahead<T, V, 2, GATE>::kSmem;
     cfg.stream = st;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension;
