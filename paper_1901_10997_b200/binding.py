@@ -266,20 +266,20 @@ def _with_reason(fn, *args):
 
 
 def lstm_linear_recurrence(a, a_t, a_b, x, x_t, x_b, h0, lengths, T, B, D, dtype, flags, h, h_t, h_b, hT, states, stream=0):
-    return _with_reason(load_library().lstm_linear_recurrence, a or None, a_t, a_b, x or None, x_t, x_b, h0 or None, lengths or None,
-                        T, B, D, dtype, flags, h or None, h_t, h_b, hT or None, states or None, stream or None)
+    return _with_reason(load_library().lstm_linear_recurrence, a, a_t, a_b, x, x_t, x_b, h0, lengths,
+                        T, B, D, dtype, flags, h, h_t, h_b, hT, states, stream)
 
 
 def lstm_linear_recurrence_backward(a, a_t, a_b, x, x_t, x_b, states, dh, dh_t, dh_b, dhT, lengths, T, B, D, dtype, flags,
                                     da, da_t, da_b, dx, dx_t, dx_b, dh0, stream=0):
-    return _with_reason(load_library().lstm_linear_recurrence_backward, a or None, a_t, a_b, x or None, x_t, x_b, states or None,
-                        dh or None, dh_t, dh_b, dhT or None, lengths or None, T, B, D, dtype, flags, da or None, da_t, da_b,
-                        dx or None, dx_t, dx_b, dh0 or None, stream or None)
+    return _with_reason(load_library().lstm_linear_recurrence_backward, a, a_t, a_b, x, x_t, x_b, states,
+                        dh, dh_t, dh_b, dhT, lengths, T, B, D, dtype, flags, da, da_t, da_b,
+                        dx, dx_t, dx_b, dh0, stream)
 
 
 def lstm_rms_norm(x, x_ld, residual, residual_ld, w, eps, rows, width, dtype, y, y_ld, scales, r, r_ld, stream=0):
-    return _with_reason(load_library().lstm_rms_norm, x or None, x_ld, residual or None, residual_ld, w or None, eps, rows, width, dtype,
-                        y or None, y_ld, scales or None, r or None, r_ld, stream or None)
+    return _with_reason(load_library().lstm_rms_norm, x, x_ld, residual, residual_ld, w, eps, rows, width, dtype,
+                        y, y_ld, scales, r, r_ld, stream)
 
 
 def lstm_rms_norm_workspace(rows, width):
@@ -288,18 +288,18 @@ def lstm_rms_norm_workspace(rows, width):
 
 
 def lstm_rms_norm_backward(dy, dy_ld, r, r_ld, w, dr, dr_ld, eps, rows, width, dtype, dx, dx_ld, dw, workspace, workspace_floats, stream=0):
-    return _with_reason(load_library().lstm_rms_norm_backward, dy or None, dy_ld, r or None, r_ld, w or None, dr or None, dr_ld, eps, rows,
-                        width, dtype, dx or None, dx_ld, dw or None, workspace or None, workspace_floats, stream or None)
+    return _with_reason(load_library().lstm_rms_norm_backward, dy, dy_ld, r, r_ld, w, dr, dr_ld, eps, rows,
+                        width, dtype, dx, dx_ld, dw, workspace, workspace_floats, stream)
 
 
 def lstm_fp8_quantize(x, x_ld, rows, width, dtype, block_rows, q, q_ld, scales, stream=0):
-    return _with_reason(load_library().lstm_fp8_quantize, x or None, x_ld, rows, width, dtype, block_rows, q or None, q_ld, scales or None,
-                        stream or None)
+    return _with_reason(load_library().lstm_fp8_quantize, x, x_ld, rows, width, dtype, block_rows, q, q_ld, scales,
+                        stream)
 
 
 def lstm_fp8_product(qx, qx_ld, sx, qw, qw_ld, sw, bias, rows, outs, width, dtype, y, y_ld, stream=0):
-    return _with_reason(load_library().lstm_fp8_product, qx or None, qx_ld, sx or None, qw or None, qw_ld, sw or None, bias or None, rows, outs,
-                        width, dtype, y or None, y_ld, stream or None)
+    return _with_reason(load_library().lstm_fp8_product, qx, qx_ld, sx, qw, qw_ld, sw, bias, rows, outs,
+                        width, dtype, y, y_ld, stream)
 
 
 # ---------------------------------------------------------------- convenience wrapper

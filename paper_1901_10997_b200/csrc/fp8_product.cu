@@ -35,6 +35,14 @@ __device__ __forceinline__ void umma_e4m3(uint32_t d_tmem, uint64_t adesc, uint6
 // instruction descriptor: fp32 sums, e4m3 x e4m3, both K-major, M x N
 __device__ constexpr uint32_t idesc_e4m3(int m, int n) { return (1u << 4) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24); }
 
+// the values of a read-back are there behind this
+__device__ __forceinline__ void tmem_arrived(uint32_t (&v)[16])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]), "+r"(v[8]), "+r"(v[9]), "+r"(v[10]),
+                   "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15])::"memory");
+}
+
 __device__ __forceinline__ uint32_t rank_in_cluster()
 {
     uint32_t r;
@@ -59,6 +67,7 @@ __device__ __forceinline__ void cluster_sync()
 // Warps 0-3 read the accumulators back (quadrant = warp), warp 4 fetches, warp 5 multiplies.
 // ---------------------------------------------------------------------------------------------------
 constexpr int kFewThreads = 192;
+constexpr int kFewSmem = 108 * 1024;
 constexpr int kMaxStages = 12;
 
 template <typename T, int R>
@@ -110,6 +119,7 @@ fp8_few_rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
                 if (++s == p.stages) { s = 0; ph ^= 1u; }
             }
         }
+        __syncwarp();
     } else if (warp == 5) {
         int s = 0;
         uint32_t ph = 0;
@@ -151,7 +161,7 @@ fp8_few_rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
             for (int c = 0; c < R; c += 16) {
                 uint32_t v[16];
                 tmem_ld16(tmem_base + ((uint32_t)(warp * 32) << 16) + (uint32_t)(buf * R + c), v);
-                asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+                tmem_arrived(v);
 #pragma unroll
                 for (int k = 0; k < 16; ++k) sum[c + k] = fmaf(__uint_as_float(v[k]), scale[buf][c + k], sum[c + k]);
             }
@@ -213,7 +223,7 @@ cudaError_t launch_few(ProductArgs &p, const CUtensorMap &mw, const CUtensorMap 
     if (p.csize > p.blocks) p.csize = p.blocks;
     constexpr int kStage = kTileOuts * kBlockK + R * kBlockK;
     // two CTAs of an SM share its memory; the sums of a split tile need the first R / 32 stages' worth
-    int stages = 108 * 1024 / kStage;
+    int stages = kFewSmem / kStage;
     if (stages > kMaxStages) stages = kMaxStages;
     const int most = (p.blocks + p.csize - 1) / p.csize, least = (R * kTileOuts * 4 + kStage - 1) / kStage;
     if (stages > most) stages = most;
@@ -230,8 +240,240 @@ cudaError_t launch_few(ProductArgs &p, const CUtensorMap &mw, const CUtensorMap 
     at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = p.csize > 1 ? 1 : 0;
-    cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg.dynamicSmemBytes);
+    static std::atomic<unsigned long long> prepared;
+    const cudaError_t e = prepare_kernel(fn, prepared, kFewSmem + 1024, false);
     if (e != cudaSuccess) return e;
+    void *args[] = {(void *)&mw, (void *)&mx, &p};
+    return cudaLaunchKernelExC(&cfg, fn, args);
+}
+
+// ---------------------------------------------------------------------------------------------------
+// Many rows of x: bound by the tensor cores, and by what brings operands to them.  A pair of CTAs (two SMs) multiplies 256 rows of x
+// by 256 rows of w at a time: each holds 128 rows of x and half of the rows of w, which the pair's instruction reads from both, so
+// that a block costs 32 KB from L2 for each 128 x 256 sums.  Rows of x are the lanes of the accumulator: a thread's sums share
+// one scale of x and one of w, one multiply-add an element.  The pairs stay and walk over the tiles.
+// Warps 0-15 read the accumulators back (quadrant = warp % 4, columns 64 (warp / 4) and on), warp 16 fetches, warp 17 of the first
+// CTA multiplies for both.
+// ---------------------------------------------------------------------------------------------------
+constexpr int kPairRows = 256, kPairOuts = 256;
+constexpr int kPairThreads = 576;
+constexpr int kPairCols = 64;                                       // columns of a warp
+constexpr int kPairStages = 5;
+constexpr uint32_t kHalfTile = 128 * kBlockK;                       // 128 rows of either operand
+constexpr int kTurn = 32 * 17;                                      // floats in which a warp turns 32 x 16 sums
+constexpr int kPairSmem = kPairStages * 2 * kHalfTile + 16 * kTurn * 4;
+
+__device__ __forceinline__ void umma_e4m3_pair(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
+}
+// arrives on the barrier at this place in both CTAs once the instructions issued so far have run
+__device__ __forceinline__ void umma_commit_pair(uint32_t bar)
+{
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)3) : "memory");
+}
+// a tile into this CTA's memory, counted by a barrier that may be the other CTA's
+__device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap *map, uint32_t bar, int x, int y)
+{
+    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+                 ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y) : "memory");
+}
+__device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar)
+{
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+// sum += v * scale, two to an instruction
+__device__ __forceinline__ void add_scaled(float &s0, float &s1, uint32_t v0, uint32_t v1, float scale)
+{
+    asm("{\n\t.reg .b64 s, v, k;\n\tmov.b64 s, {%0, %1};\n\tmov.b64 v, {%2, %3};\n\tmov.b64 k, {%4, %4};\n\t"
+        "fma.rn.f32x2 s, v, k, s;\n\tmov.b64 {%0, %1}, s;\n\t}"
+        : "+f"(s0), "+f"(s1) : "r"(v0), "r"(v1), "f"(scale));
+}
+
+template <typename T>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
+fp8_many_rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x, const __grid_constant__ ProductArgs p)
+{
+    extern __shared__ __align__(16) unsigned char smem_raw[];
+    __shared__ __align__(8) unsigned long long full_bar[kPairStages], empty_bar[kPairStages], sums_full[2], sums_empty[2];
+    __shared__ uint32_t tmem_base_s;
+    __shared__ int abort_s;
+
+    const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
+    const int rank = (int)rank_in_cluster();
+    const uint32_t tiles = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    const int n_tiles = (p.outs + kPairOuts - 1) / kPairOuts;
+    const long long all = (long long)n_tiles * ((p.rows + kPairRows - 1) / kPairRows);
+    const int pairs = gridDim.x / 2, pair = blockIdx.x / 2;
+
+    if (tid == 0) {
+        abort_s = 0;
+        for (int s = 0; s < kPairStages; ++s) { mbar_init(smem_u32(&full_bar[s]), 1); mbar_init(smem_u32(&empty_bar[s]), 1); }
+        for (int s = 0; s < 2; ++s) { mbar_init(smem_u32(&sums_full[s]), 1); mbar_init(smem_u32(&sums_empty[s]), 32); }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (warp == 17) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base_s)), "r"(512u) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    cluster_sync();                                      // both CTAs' barriers and tensor memory are there
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem_base = tmem_base_s;
+    volatile int *abort_flag = &abort_s;
+
+    if (warp == 16) {
+        if (lane == 0) {
+            int s = 0;
+            uint32_t ph = 0;
+            bool ok = true;
+            for (long long tile = pair; tile < all && ok; tile += pairs) {
+                const int m0 = (int)(tile / n_tiles) * kPairRows + rank * 128, n0 = (int)(tile % n_tiles) * kPairOuts + rank * 128;
+                for (int j = 0; j < p.blocks; ++j) {
+                    if (!(ok = mbar_wait(smem_u32(&empty_bar[s]), ph ^ 1u, abort_flag))) break;
+                    const uint32_t at = tiles + (uint32_t)s * 2 * kHalfTile, fb = at_rank(smem_u32(&full_bar[s]), 0);
+                    if (rank == 0) mbar_expect_tx(smem_u32(&full_bar[s]), 4 * kHalfTile);      // both CTAs' tiles
+                    tma_load_2d_pair(at, &map_x, fb, j * kBlockK, m0);
+                    tma_load_2d_pair(at + kHalfTile, &map_w, fb, j * kBlockK, n0);
+                    if (++s == kPairStages) { s = 0; ph ^= 1u; }
+                }
+            }
+        }
+        __syncwarp();
+    } else if (warp == 17) {
+        if (rank == 0) {
+            int s = 0;
+            uint32_t ph = 0;
+            long long i = 0;
+            bool ok = true;
+            for (long long tile = pair; tile < all && ok; tile += pairs) {
+                for (int j = 0; j < p.blocks; ++j, ++i) {
+                    const int buf = (int)(i & 1);
+                    ok = mbar_wait(smem_u32(&sums_empty[buf]), (uint32_t)((i >> 1) & 1) ^ 1u, abort_flag);
+                    ok = ok && mbar_wait(smem_u32(&full_bar[s]), ph, abort_flag);
+                    if (!(ok = __all_sync(0xffffffffu, ok))) break;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    const uint32_t at = tiles + (uint32_t)s * 2 * kHalfTile;
+                    const uint64_t xdesc = umma_desc_sw128(at), wdesc = umma_desc_sw128(at + kHalfTile);
+                    if (elect_one()) {
+#pragma unroll
+                        for (int k = 0; k < kBlockK / 32; ++k)
+                            umma_e4m3_pair(tmem_base + buf * kPairOuts, xdesc + 2 * k, wdesc + 2 * k, idesc_e4m3(kPairRows, kPairOuts), k > 0);
+                        umma_commit_pair(smem_u32(&empty_bar[s]));
+                        umma_commit_pair(smem_u32(&sums_full[buf]));
+                    }
+                    __syncwarp();
+                    if (++s == kPairStages) { s = 0; ph ^= 1u; }
+                }
+            }
+        }
+    } else if (warp < 16) {
+        const int quad = warp & 3, part = warp >> 2;
+        const uint32_t lanes = (uint32_t)(quad * 32) << 16;
+        float *turn = reinterpret_cast<float *>(smem_raw + (tiles - smem_u32(smem_raw)) + kPairStages * 2 * kHalfTile) + warp * kTurn;
+        T *y = (T *)p.y;
+        const bool even = p.y_ld % 2 == 0 && (unsigned long long)y % (2 * sizeof(T)) == 0;
+        const uint32_t empty0 = at_rank(smem_u32(&sums_empty[0]), 0), empty1 = at_rank(smem_u32(&sums_empty[1]), 0);
+        long long i = 0;
+        bool ok = true;
+        for (long long tile = pair; tile < all; tile += pairs) {
+            const int m0 = (int)(tile / n_tiles) * kPairRows + rank * 128 + quad * 32, n0 = (int)(tile % n_tiles) * kPairOuts + part * kPairCols;
+            const bool mine = m0 + lane < p.rows, any = n0 < p.outs;
+            const float *sx = p.sx + (long long)(mine ? m0 + lane : 0) * p.blocks, *sw = p.sw + (long long)(any ? n0 / kTileOuts : 0) * p.blocks;
+            float sum[kPairCols];
+#pragma unroll
+            for (int c = 0; c < kPairCols; ++c) sum[c] = 0.0f;
+            float next = sx[0] * sw[0];
+            for (int j = 0; j < p.blocks; ++j, ++i) {
+                const int buf = (int)(i & 1);
+                const float scale = next;
+                if (j + 1 < p.blocks) next = sx[j + 1] * sw[j + 1];
+                ok = ok && mbar_wait(smem_u32(&sums_full[buf]), (uint32_t)((i >> 1) & 1), abort_flag);
+                __syncwarp();
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                const uint32_t from = tmem_base + lanes + (uint32_t)(buf * kPairOuts + part * kPairCols);
+                uint32_t v[2][16];
+                tmem_ld16(from, v[0]);
+#pragma unroll
+                for (int c = 0; c < kPairCols; c += 16) {
+                    const int now = c / 16 & 1;
+                    tmem_arrived(v[now]);
+                    if (c + 16 < kPairCols) tmem_ld16(from + c + 16, v[now ^ 1]);
+                    else {
+                        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive_cluster(buf ? empty1 : empty0);
+                    }
+#pragma unroll
+                    for (int k = 0; k < 16; k += 2) add_scaled(sum[c + k], sum[c + k + 1], v[now][k], v[now][k + 1], scale);
+                }
+            }
+            if (!ok) {
+#pragma unroll
+                for (int c = 0; c < kPairCols; ++c) sum[c] = __uint_as_float(0x7fffffffu);
+            }
+            // a thread has a row, memory wants columns side by side: 32 x 16 sums at a time change places within the warp
+#pragma unroll
+            for (int c0 = 0; c0 < kPairCols; c0 += 16) {
+                if (n0 + c0 >= p.outs || m0 >= p.rows) break;
+                __syncwarp();
+#pragma unroll
+                for (int c = 0; c < 16; ++c) turn[lane * 17 + c] = sum[c0 + c];
+                __syncwarp();
+                const int rows = min(32, p.rows - m0);
+                if (even) {
+                    const int n = n0 + c0 + 2 * (lane & 7), r0 = lane >> 3;
+                    const float b0 = p.bias && n < p.outs ? p.bias[n] : 0.0f, b1 = p.bias && n + 1 < p.outs ? p.bias[n + 1] : 0.0f;
+                    T *out = y + (long long)(m0 + r0) * p.y_ld + n;
+                    const float *in = turn + r0 * 17 + 2 * (lane & 7);
+#pragma unroll
+                    for (int r = 0; r < 32; r += 4, out += 4 * p.y_ld, in += 4 * 17) {
+                        if (r0 + r >= rows) break;
+                        const float o[2] = {in[0] + b0, in[1] + b1};
+                        if (n + 1 < p.outs) store_vec<T, 2>(out, o);
+                        else if (n < p.outs) out[0] = T(o[0]);
+                    }
+                } else {
+                    const int n = n0 + c0 + (lane & 15), r0 = lane >> 4;
+                    const float b = p.bias && n < p.outs ? p.bias[n] : 0.0f;
+                    T *out = y + (long long)(m0 + r0) * p.y_ld + n;
+                    const float *in = turn + r0 * 17 + (lane & 15);
+#pragma unroll 4
+                    for (int r = r0; r < rows; r += 2, out += 2 * p.y_ld, in += 2 * 17)
+                        if (n < p.outs) out[0] = T(in[0] + b);
+                }
+            }
+        }
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    cluster_sync();                                      // no barrier and no operand goes while the other CTA needs it
+    if (warp == 17) {
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512u) : "memory");
+    }
+}
+
+template <typename T>
+cudaError_t launch_many(ProductArgs &p, const CUtensorMap &mw, const CUtensorMap &mx, int sms, cudaStream_t st)
+{
+    const void *fn = (const void *)fp8_many_rows_kernel<T>;
+    static std::atomic<unsigned long long> prepared;
+    const cudaError_t e = prepare_kernel(fn, prepared, kPairSmem + 1024, false);
+    if (e != cudaSuccess) return e;
+    const long long tiles = (long long)((p.outs + kPairOuts - 1) / kPairOuts) * ((p.rows + kPairRows - 1) / kPairRows);
+    const int pairs = (int)(tiles < sms / 2 ? tiles : sms / 2);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(2 * pairs));
+    cfg.blockDim = dim3(kPairThreads);
+    cfg.dynamicSmemBytes = kPairSmem + 1024;
+    cfg.stream = st;
     void *args[] = {(void *)&mw, (void *)&mx, &p};
     return cudaLaunchKernelExC(&cfg, fn, args);
 }
@@ -240,10 +482,12 @@ template <typename T>
 cudaError_t launch(ProductArgs &p, const void *qx, long long qx_ld, const void *qw, long long qw_ld, int width, int sms, cudaStream_t st, bool &mapped)
 {
     const int R = p.rows <= 16 ? 16 : p.rows <= 32 ? 32 : p.rows <= 64 ? 64 : 128;
+    const bool many = p.rows > 128;
     CUtensorMap mw, mx;
     mapped = encode_tmap_2d(&mw, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, qw, p.outs, width, qw_ld, kTileOuts) &&
              encode_tmap_2d(&mx, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, qx, p.rows, width, qx_ld, R);
     if (!mapped) return cudaErrorInvalidValue;
+    if (many) return launch_many<T>(p, mw, mx, sms, st);
     if (R == 16) return launch_few<T, 16>(p, mw, mx, sms, st);
     if (R == 32) return launch_few<T, 32>(p, mw, mx, sms, st);
     if (R == 64) return launch_few<T, 64>(p, mw, mx, sms, st);

@@ -674,8 +674,8 @@ cudaError_t launch(LinrecArgs &p, bool backward, int sms, cudaStream_t st)
     at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = csize > 1 ? 1 : 0;
-    cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg.dynamicSmemBytes);
-    if (e == cudaSuccess && csize > 8) e = cudaFuncSetAttribute(fn, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    static std::atomic<unsigned long long> prepared[2];
+    const cudaError_t e = prepare_kernel(fn, prepared[backward], (int)cfg.dynamicSmemBytes, true);
     if (e != cudaSuccess) return e;
     void *args[] = {&p};
     return cudaLaunchKernelExC(&cfg, fn, args);

@@ -41,6 +41,20 @@ inline int device_sms(int &sms, const Failure &fail)
     return LSTM_OK;
 }
 
+// The attributes that a kernel needs once on each device; `done` is the kernel's own, a bit for each device.
+inline cudaError_t prepare_kernel(const void *fn, std::atomic<unsigned long long> &done, int dynamic_smem, bool large_clusters)
+{
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    const unsigned long long bit = dev < 64 ? 1ull << dev : 0;
+    if (done.load(std::memory_order_acquire) & bit) return cudaSuccess;
+    e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, dynamic_smem);
+    if (e == cudaSuccess && large_clusters) e = cudaFuncSetAttribute(fn, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_release);
+    return e;
+}
+
 // ---------------------------------------------------------------------------------------------------
 // V elements of type T (float or __nv_bfloat16), loaded and stored as one word of up to 16 bytes
 // ---------------------------------------------------------------------------------------------------
