@@ -147,13 +147,13 @@ fp8_few_rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
         for (int r = 0; r < R; ++r) sum[r] = 0.0f;
         const bool mine = tid < R && m0 + tid < p.rows;
         const float *sx = p.sx + (long long)(m0 + tid) * p.blocks + j0, *sw = p.sw + (long long)n_tile * p.blocks + j0;
-        float next = mine && nj > 0 ? sx[0] * sw[0] : 0.0f;
+        float next_x = mine && nj > 0 ? sx[0] : 0.0f, next_w = nj > 0 ? sw[0] : 0.0f;
         bool ok = true;
         for (int i = 0; i < nj; ++i) {
             const int buf = i & 1;
-            if (tid < R) scale[buf][tid] = next;
+            if (tid < R) scale[buf][tid] = next_x * next_w;
             bar_sync(1, 128);                            // the other buffer is written next when all have left it
-            if (mine && i + 1 < nj) next = sx[i + 1] * sw[i + 1];
+            if (mine && i + 1 < nj) { next_x = sx[i + 1]; next_w = sw[i + 1]; }
             ok = mbar_wait(smem_u32(&sums_full[buf]), (i >> 1) & 1, abort_flag) && ok;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             __syncwarp();
@@ -253,15 +253,18 @@ cudaError_t launch_few(ProductArgs &p, const CUtensorMap &mw, const CUtensorMap 
 // that a block costs 32 KB from L2 for each 128 x 256 sums.  Rows of x are the lanes of the accumulator: a thread's sums share
 // one scale of x and one of w, one multiply-add an element.  The pairs stay and walk over the tiles.
 // Warps 0-15 read the accumulators back (quadrant = warp % 4, columns 64 (warp / 4) and on), warp 16 fetches, warp 17 of the first
-// CTA multiplies for both.
+// CTA multiplies for both, warps 18 and 19 bring the scales of the rows of x, which lie a row's length apart, 16 blocks at a time into
+// shared memory (each reading warp on its own would touch 32 lines a block).
 // ---------------------------------------------------------------------------------------------------
 constexpr int kPairRows = 256, kPairOuts = 256;
-constexpr int kPairThreads = 576;
+constexpr int kPairThreads = 640;
 constexpr int kPairCols = 64;                                       // columns of a warp
-constexpr int kPairStages = 5;
+constexpr int kPairStages = 4;
 constexpr uint32_t kHalfTile = 128 * kBlockK;                       // 128 rows of either operand
-constexpr int kTurn = 32 * 17;                                      // floats in which a warp turns 32 x 16 sums
-constexpr int kPairSmem = kPairStages * 2 * kHalfTile + 16 * kTurn * 4;
+constexpr int kTurnPitch = 34, kTurn = 32 * kTurnPitch;             // words in which a warp turns 32 rows of 32 words (64 bf16 or 32 fp32)
+constexpr int kScaleBlocks = 16, kScalePitch = 130;                 // scales staged at once, [block][row]: eight rows x four words without conflicts
+constexpr int kScales = kScaleBlocks * kScalePitch + kPairOuts;     // and the tile's biases
+constexpr int kPairSmem = kPairStages * 2 * kHalfTile + (16 * kTurn + 2 * kScales) * 4;
 
 __device__ __forceinline__ void umma_e4m3_pair(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate)
 {
@@ -299,7 +302,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
 fp8_many_rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x, const __grid_constant__ ProductArgs p)
 {
     extern __shared__ __align__(16) unsigned char smem_raw[];
-    __shared__ __align__(8) unsigned long long full_bar[kPairStages], empty_bar[kPairStages], sums_full[2], sums_empty[2];
+    __shared__ __align__(8) unsigned long long full_bar[kPairStages], empty_bar[kPairStages], sums_full[2], sums_empty[2], scales_full[2], scales_empty[2];
     __shared__ uint32_t tmem_base_s;
     __shared__ int abort_s;
 
@@ -314,6 +317,7 @@ fp8_many_rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
         abort_s = 0;
         for (int s = 0; s < kPairStages; ++s) { mbar_init(smem_u32(&full_bar[s]), 1); mbar_init(smem_u32(&empty_bar[s]), 1); }
         for (int s = 0; s < 2; ++s) { mbar_init(smem_u32(&sums_full[s]), 1); mbar_init(smem_u32(&sums_empty[s]), 32); }
+        for (int s = 0; s < 2; ++s) { mbar_init(smem_u32(&scales_full[s]), 64); mbar_init(smem_u32(&scales_empty[s]), 16); }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
@@ -327,8 +331,37 @@ fp8_many_rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem_base = tmem_base_s;
     volatile int *abort_flag = &abort_s;
+    float *staged = reinterpret_cast<float *>(smem_raw + (tiles - smem_u32(smem_raw)) + kPairStages * 2 * kHalfTile);
 
-    if (warp == 16) {
+    if (warp >= 18) {
+        // rows 64 (warp - 18) and on: lane = row of eight, word of four
+        int c = 0;
+        bool ok = true;
+        for (long long tile = pair; tile < all && ok; tile += pairs) {
+            const int m0 = (int)(tile / n_tiles) * kPairRows + rank * 128, r0 = (warp - 18) * 64 + (lane >> 2);
+            for (int j0 = 0; j0 < p.blocks; j0 += kScaleBlocks, ++c) {
+                if (!(ok = mbar_wait(smem_u32(&scales_empty[c & 1]), (uint32_t)((c >> 1) & 1) ^ 1u, abort_flag))) break;
+                float *to = staged + (c & 1) * kScales;
+#pragma unroll 2
+                for (int r = r0; r < r0 + 64; r += 8) {
+                    const float *from = p.sx + (long long)(m0 + r) * p.blocks;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const int j = 4 * (lane & 3) + k;
+                        to[j * kScalePitch + r] = m0 + r < p.rows && j0 + j < p.blocks ? from[j0 + j] : 0.0f;
+                    }
+                }
+                if (warp == 18 && j0 + kScaleBlocks >= p.blocks) {        // the biases come with a tile's last scales
+                    const int n0 = (int)(tile % n_tiles) * kPairOuts;
+#pragma unroll
+                    for (int n = lane; n < kPairOuts; n += 32)
+                        to[kScaleBlocks * kScalePitch + n] = p.bias && n0 + n < p.outs ? p.bias[n0 + n] : 0.0f;
+                }
+                mbar_arrive(smem_u32(&scales_full[c & 1]));
+            }
+        }
+        __syncwarp();
+    } else if (warp == 16) {
         if (lane == 0) {
             int s = 0;
             uint32_t ph = 0;
@@ -373,27 +406,40 @@ fp8_many_rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
                 }
             }
         }
-    } else if (warp < 16) {
+    } else {
         const int quad = warp & 3, part = warp >> 2;
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;
-        float *turn = reinterpret_cast<float *>(smem_raw + (tiles - smem_u32(smem_raw)) + kPairStages * 2 * kHalfTile) + warp * kTurn;
+        uint32_t *turn = reinterpret_cast<uint32_t *>(staged + 2 * kScales) + warp * kTurn;
         T *y = (T *)p.y;
-        const bool even = p.y_ld % 2 == 0 && (unsigned long long)y % (2 * sizeof(T)) == 0;
+        constexpr int kWord = 4 / sizeof(T);                        // columns of a word
+        // words that may be stored at once: two, one, or (rows of bf16 that start anywhere) half of one
+        const unsigned long long off = (unsigned long long)y | (unsigned long long)p.y_ld * sizeof(T);
+        const int wide = off % 8 == 0 ? 2 : off % 4 == 0 ? 1 : 0;
         const uint32_t empty0 = at_rank(smem_u32(&sums_empty[0]), 0), empty1 = at_rank(smem_u32(&sums_empty[1]), 0);
+        int chunk = 0;
         long long i = 0;
         bool ok = true;
         for (long long tile = pair; tile < all; tile += pairs) {
             const int m0 = (int)(tile / n_tiles) * kPairRows + rank * 128 + quad * 32, n0 = (int)(tile % n_tiles) * kPairOuts + part * kPairCols;
-            const bool mine = m0 + lane < p.rows, any = n0 < p.outs;
-            const float *sx = p.sx + (long long)(mine ? m0 + lane : 0) * p.blocks, *sw = p.sw + (long long)(any ? n0 / kTileOuts : 0) * p.blocks;
+            const float *sw = p.sw + (long long)(n0 < p.outs ? n0 / kTileOuts : 0) * p.blocks, *sx = nullptr;
             float sum[kPairCols];
 #pragma unroll
             for (int c = 0; c < kPairCols; ++c) sum[c] = 0.0f;
-            float next = sx[0] * sw[0];
+            float next_w = sw[0];
             for (int j = 0; j < p.blocks; ++j, ++i) {
                 const int buf = (int)(i & 1);
-                const float scale = next;
-                if (j + 1 < p.blocks) next = sx[j + 1] * sw[j + 1];
+                if (j % kScaleBlocks == 0) {
+                    if (j) {
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(smem_u32(&scales_empty[chunk & 1]));
+                        ++chunk;
+                    }
+                    ok = ok && mbar_wait(smem_u32(&scales_full[chunk & 1]), (uint32_t)((chunk >> 1) & 1), abort_flag);
+                    sx = staged + (chunk & 1) * kScales + quad * 32 + lane;
+                }
+                const float scale = *sx * next_w;
+                sx += kScalePitch;
+                if (j + 1 < p.blocks) next_w = sw[j + 1];
                 ok = ok && mbar_wait(smem_u32(&sums_full[buf]), (uint32_t)((i >> 1) & 1), abort_flag);
                 __syncwarp();
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -418,35 +464,47 @@ fp8_many_rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
 #pragma unroll
                 for (int c = 0; c < kPairCols; ++c) sum[c] = __uint_as_float(0x7fffffffu);
             }
-            // a thread has a row, memory wants columns side by side: 32 x 16 sums at a time change places within the warp
+            const float *bias = staged + (chunk & 1) * kScales + kScaleBlocks * kScalePitch + part * kPairCols;
 #pragma unroll
-            for (int c0 = 0; c0 < kPairCols; c0 += 16) {
-                if (n0 + c0 >= p.outs || m0 >= p.rows) break;
+            for (int c = 0; c < kPairCols; c += 4) {
+                const float4 b = *reinterpret_cast<const float4 *>(bias + c);
+                sum[c] += b.x; sum[c + 1] += b.y; sum[c + 2] += b.z; sum[c + 3] += b.w;
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&scales_empty[chunk & 1]));
+            ++chunk;
+            // a thread has a row, memory wants columns side by side: 32 x 32 words at a time change places within the warp
+            const int rows = min(32, p.rows - m0);
+#pragma unroll
+            for (int c0 = 0; c0 < kPairCols; c0 += 32 * kWord) {
+                const int left = p.outs - n0 - c0;
+                if (left <= 0 || rows <= 0) break;
                 __syncwarp();
 #pragma unroll
-                for (int c = 0; c < 16; ++c) turn[lane * 17 + c] = sum[c0 + c];
-                __syncwarp();
-                const int rows = min(32, p.rows - m0);
-                if (even) {
-                    const int n = n0 + c0 + 2 * (lane & 7), r0 = lane >> 3;
-                    const float b0 = p.bias && n < p.outs ? p.bias[n] : 0.0f, b1 = p.bias && n + 1 < p.outs ? p.bias[n + 1] : 0.0f;
-                    T *out = y + (long long)(m0 + r0) * p.y_ld + n;
-                    const float *in = turn + r0 * 17 + 2 * (lane & 7);
+                for (int w = 0; w < 32; w += 2) {
+                    Vec<T, 2 * kWord> v;
 #pragma unroll
-                    for (int r = 0; r < 32; r += 4, out += 4 * p.y_ld, in += 4 * 17) {
-                        if (r0 + r >= rows) break;
-                        const float o[2] = {in[0] + b0, in[1] + b1};
-                        if (n + 1 < p.outs) store_vec<T, 2>(out, o);
-                        else if (n < p.outs) out[0] = T(o[0]);
-                    }
+                    for (int c = 0; c < 2 * kWord; ++c) v.e[c] = T(sum[c0 + w * kWord + c]);
+                    *reinterpret_cast<Vec<T, 2 * kWord> *>(turn + lane * kTurnPitch + w) = v;
+                }
+                __syncwarp();
+                T *out = y + (long long)m0 * p.y_ld + n0 + c0;
+                if (wide == 2 && left >= 32 * kWord) {
+                    const int w = 2 * (lane & 15), r0 = lane >> 4;
+                    out += r0 * p.y_ld + w * kWord;
+#pragma unroll
+                    for (int r = 0; r < 32; r += 2, out += 2 * p.y_ld)
+                        if (r + r0 < rows) *reinterpret_cast<uint2 *>(out) = *reinterpret_cast<const uint2 *>(turn + (r + r0) * kTurnPitch + w);
+                } else if (wide && left >= 32 * kWord) {
+                    out += lane * kWord;
+#pragma unroll 8
+                    for (int r = 0; r < rows; ++r, out += p.y_ld) *reinterpret_cast<uint32_t *>(out) = turn[r * kTurnPitch + lane];
                 } else {
-                    const int n = n0 + c0 + (lane & 15), r0 = lane >> 4;
-                    const float b = p.bias && n < p.outs ? p.bias[n] : 0.0f;
-                    T *out = y + (long long)(m0 + r0) * p.y_ld + n;
-                    const float *in = turn + r0 * 17 + (lane & 15);
-#pragma unroll 4
-                    for (int r = r0; r < rows; r += 2, out += 2 * p.y_ld, in += 2 * 17)
-                        if (n < p.outs) out[0] = T(in[0] + b);
+                    for (int c = lane; c < 32 * kWord && c < left; c += 32) {
+                        T *o = out + c;
+#pragma unroll 8
+                        for (int r = 0; r < rows; ++r, o += p.y_ld) *o = reinterpret_cast<const T *>(turn + r * kTurnPitch)[c];
+                    }
                 }
             }
         }
