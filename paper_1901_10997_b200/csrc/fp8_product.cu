@@ -35,6 +35,17 @@ __device__ __forceinline__ void umma_e4m3(uint32_t d_tmem, uint64_t adesc, uint6
 // instruction descriptor: fp32 sums, e4m3 x e4m3, both K-major, M x N
 __device__ constexpr uint32_t idesc_e4m3(int m, int n) { return (1u << 4) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24); }
 
+// mbar_wait by warps that have nothing else to do: each try may sleep for some microseconds, so that they leave the scheduler to others
+__device__ __forceinline__ bool wait_long(uint32_t bar, uint32_t parity, volatile int *abort_flag)
+{
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok) : "r"(bar), "r"(parity), "r"(10000u) : "memory");
+    return ok ? true : mbar_wait(bar, parity, abort_flag);
+}
 // the values of a read-back are there behind this
 __device__ __forceinline__ void tmem_arrived(uint32_t (&v)[16])
 {
@@ -251,8 +262,10 @@ cudaError_t launch_few(ProductArgs &p, const CUtensorMap &mw, const CUtensorMap 
 // Many rows of x: bound by the tensor cores, and by what brings operands to them.  A pair of CTAs (two SMs) multiplies 256 rows of x
 // by 256 rows of w at a time: each holds 128 rows of x and half of the rows of w, which the pair's instruction reads from both, so
 // that a block costs 32 KB from L2 for each 128 x 256 sums.  Rows of x are the lanes of the accumulator: a thread's sums share
-// one scale of x and one of w, one multiply-add an element.  The pairs stay and walk over the tiles.
-// Warps 0-15 read the accumulators back (quadrant = warp % 4, columns 64 (warp / 4) and on), warp 16 fetches, warp 17 of the first
+// one scale of x and one of w, one multiply-add an element.  The pairs stay and walk over the tiles.  A block is multiplied in two
+// halves of its columns with barriers of their own, so that four accumulators are on their way between the tensor cores and
+// the warps that read them.
+// Warps 0-15 read the accumulators back (quadrant = warp % 4, 64 columns each), warp 16 fetches, warp 17 of the first
 // CTA multiplies for both, warps 18 and 19 bring the scales of the rows of x, which lie a row's length apart, 16 blocks at a time into
 // shared memory (each reading warp on its own would touch 32 lines a block).
 // ---------------------------------------------------------------------------------------------------
@@ -302,7 +315,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
 fp8_many_rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x, const __grid_constant__ ProductArgs p)
 {
     extern __shared__ __align__(16) unsigned char smem_raw[];
-    __shared__ __align__(8) unsigned long long full_bar[kPairStages], empty_bar[kPairStages], sums_full[2], sums_empty[2], scales_full[2], scales_empty[2];
+    __shared__ __align__(8) unsigned long long full_bar[kPairStages], empty_bar[kPairStages], sums_full[4], sums_empty[4], scales_full[2], scales_empty[2];
     __shared__ uint32_t tmem_base_s;
     __shared__ int abort_s;
 
@@ -316,7 +329,7 @@ fp8_many_rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
     if (tid == 0) {
         abort_s = 0;
         for (int s = 0; s < kPairStages; ++s) { mbar_init(smem_u32(&full_bar[s]), 1); mbar_init(smem_u32(&empty_bar[s]), 1); }
-        for (int s = 0; s < 2; ++s) { mbar_init(smem_u32(&sums_full[s]), 1); mbar_init(smem_u32(&sums_empty[s]), 32); }
+        for (int s = 0; s < 4; ++s) { mbar_init(smem_u32(&sums_full[s]), 1); mbar_init(smem_u32(&sums_empty[s]), 16); }
         for (int s = 0; s < 2; ++s) { mbar_init(smem_u32(&scales_full[s]), 64); mbar_init(smem_u32(&scales_empty[s]), 16); }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -351,7 +364,7 @@ fp8_many_rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
                         to[j * kScalePitch + r] = m0 + r < p.rows && j0 + j < p.blocks ? from[j0 + j] : 0.0f;
                     }
                 }
-                if (warp == 18 && j0 + kScaleBlocks >= p.blocks) {        // the biases come with a tile's last scales
+                if (warp == 18 && j0 == 0) {             // the biases come with a tile's first scales
                     const int n0 = (int)(tile % n_tiles) * kPairOuts;
 #pragma unroll
                     for (int n = lane; n < kPairOuts; n += 32)
@@ -388,26 +401,33 @@ fp8_many_rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
             for (long long tile = pair; tile < all && ok; tile += pairs) {
                 for (int j = 0; j < p.blocks; ++j, ++i) {
                     const int buf = (int)(i & 1);
-                    ok = mbar_wait(smem_u32(&sums_empty[buf]), (uint32_t)((i >> 1) & 1) ^ 1u, abort_flag);
-                    ok = ok && mbar_wait(smem_u32(&full_bar[s]), ph, abort_flag);
-                    if (!(ok = __all_sync(0xffffffffu, ok))) break;
-                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    if (!(ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&full_bar[s]), ph, abort_flag)))) break;
                     const uint32_t at = tiles + (uint32_t)s * 2 * kHalfTile;
                     const uint64_t xdesc = umma_desc_sw128(at), wdesc = umma_desc_sw128(at + kHalfTile);
-                    if (elect_one()) {
 #pragma unroll
-                        for (int k = 0; k < kBlockK / 32; ++k)
-                            umma_e4m3_pair(tmem_base + buf * kPairOuts, xdesc + 2 * k, wdesc + 2 * k, idesc_e4m3(kPairRows, kPairOuts), k > 0);
-                        umma_commit_pair(smem_u32(&empty_bar[s]));
-                        umma_commit_pair(smem_u32(&sums_full[buf]));
+                    for (int half = 0; half < 2 && ok; ++half) {
+                        const int set = 2 * buf + half;
+                        if (!(ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sums_empty[set]), (uint32_t)((i >> 1) & 1) ^ 1u, abort_flag)))) break;
+                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                        if (elect_one()) {
+#pragma unroll
+                            for (int k = 0; k < kBlockK / 32; ++k)
+                                umma_e4m3_pair(tmem_base + set * (kPairOuts / 2), xdesc + 2 * k, wdesc + half * (kHalfTile / 2 / 16) + 2 * k,
+                                               idesc_e4m3(kPairRows, kPairOuts / 2), k > 0);
+                            if (half == 1) umma_commit_pair(smem_u32(&empty_bar[s]));
+                            umma_commit_pair(smem_u32(&sums_full[set]));
+                        }
+                        __syncwarp();
                     }
+                    if (!ok) break;
                     __syncwarp();
                     if (++s == kPairStages) { s = 0; ph ^= 1u; }
                 }
             }
         }
     } else {
-        const int quad = warp & 3, part = warp >> 2;
+        // a half's 128 columns of tensor memory are 64 rows of w from each CTA
+        const int quad = warp & 3, part = warp >> 2, col0 = (part & 1) * 128 + (part >> 1) * 64;
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;
         uint32_t *turn = reinterpret_cast<uint32_t *>(staged + 2 * kScales) + warp * kTurn;
         T *y = (T *)p.y;
@@ -415,64 +435,60 @@ fp8_many_rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
         // words that may be stored at once: two, one, or (rows of bf16 that start anywhere) half of one
         const unsigned long long off = (unsigned long long)y | (unsigned long long)p.y_ld * sizeof(T);
         const int wide = off % 8 == 0 ? 2 : off % 4 == 0 ? 1 : 0;
-        const uint32_t empty0 = at_rank(smem_u32(&sums_empty[0]), 0), empty1 = at_rank(smem_u32(&sums_empty[1]), 0);
+        // this half's barriers: of the accumulators of even blocks, those of odd ones 16 bytes on
+        const uint32_t full_at = smem_u32(&sums_full[part >> 1]), empty_at = at_rank(smem_u32(&sums_empty[part >> 1]), 0);
+        // columns of tensor memory: buffer, half, the warp's 64
+        const uint32_t from0 = tmem_base + lanes + (uint32_t)(part * kPairCols);
         int chunk = 0;
-        long long i = 0;
+        uint32_t i = 0;
         bool ok = true;
         for (long long tile = pair; tile < all; tile += pairs) {
-            const int m0 = (int)(tile / n_tiles) * kPairRows + rank * 128 + quad * 32, n0 = (int)(tile % n_tiles) * kPairOuts + part * kPairCols;
-            const float *sw = p.sw + (long long)(n0 < p.outs ? n0 / kTileOuts : 0) * p.blocks, *sx = nullptr;
-            float sum[kPairCols];
+            const int m0 = (int)(tile / n_tiles) * kPairRows + rank * 128 + quad * 32, n0 = (int)(tile % n_tiles) * kPairOuts + col0;
+            const float *sw = p.sw + (long long)(n0 < p.outs ? n0 / kTileOuts : 0) * p.blocks;
+            float sum[kPairCols], next_w = sw[0];
+            for (int j0 = 0; j0 < p.blocks; j0 += kScaleBlocks, ++chunk) {
+                ok = wait_long(smem_u32(&scales_full[chunk & 1]), (uint32_t)((chunk >> 1) & 1), abort_flag) && ok;
+                const float *sx = staged + (chunk & 1) * kScales + quad * 32 + lane;
+                if (j0 == 0) {
+                    const float *bias = staged + (chunk & 1) * kScales + kScaleBlocks * kScalePitch + col0;
 #pragma unroll
-            for (int c = 0; c < kPairCols; ++c) sum[c] = 0.0f;
-            float next_w = sw[0];
-            for (int j = 0; j < p.blocks; ++j, ++i) {
-                const int buf = (int)(i & 1);
-                if (j % kScaleBlocks == 0) {
-                    if (j) {
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(smem_u32(&scales_empty[chunk & 1]));
-                        ++chunk;
+                    for (int c = 0; c < kPairCols; c += 4) {
+                        const float4 b = *reinterpret_cast<const float4 *>(bias + c);
+                        sum[c] = b.x; sum[c + 1] = b.y; sum[c + 2] = b.z; sum[c + 3] = b.w;
                     }
-                    ok = ok && mbar_wait(smem_u32(&scales_full[chunk & 1]), (uint32_t)((chunk >> 1) & 1), abort_flag);
-                    sx = staged + (chunk & 1) * kScales + quad * 32 + lane;
                 }
-                const float scale = *sx * next_w;
-                sx += kScalePitch;
-                if (j + 1 < p.blocks) next_w = sw[j + 1];
-                ok = ok && mbar_wait(smem_u32(&sums_full[buf]), (uint32_t)((i >> 1) & 1), abort_flag);
+                const int j1 = min(j0 + kScaleBlocks, p.blocks);
+                for (int j = j0; j < j1; ++j, ++i, sx += kScalePitch) {
+                    const float scale = *sx * next_w;
+                    if (j + 1 < p.blocks) next_w = sw[j + 1];
+                    const uint32_t set = 2 * (i & 1);
+                    ok = wait_long(full_at + 8 * set, (i >> 1) & 1, abort_flag) && ok;
+                    __syncwarp();
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    const uint32_t from = from0 + set * (kPairOuts / 2);
+                    uint32_t v[2][16];
+                    tmem_ld16(from, v[0]);
+#pragma unroll
+                    for (int c = 0; c < kPairCols; c += 16) {
+                        const int now = c / 16 & 1;
+                        tmem_arrived(v[now]);
+                        if (c + 16 < kPairCols) tmem_ld16(from + c + 16, v[now ^ 1]);
+                        else {
+                            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive_cluster(empty_at + 8 * set);
+                        }
+#pragma unroll
+                        for (int k = 0; k < 16; k += 2) add_scaled(sum[c + k], sum[c + k + 1], v[now][k], v[now][k + 1], scale);
+                    }
+                }
                 __syncwarp();
-                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const uint32_t from = tmem_base + lanes + (uint32_t)(buf * kPairOuts + part * kPairCols);
-                uint32_t v[2][16];
-                tmem_ld16(from, v[0]);
-#pragma unroll
-                for (int c = 0; c < kPairCols; c += 16) {
-                    const int now = c / 16 & 1;
-                    tmem_arrived(v[now]);
-                    if (c + 16 < kPairCols) tmem_ld16(from + c + 16, v[now ^ 1]);
-                    else {
-                        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive_cluster(buf ? empty1 : empty0);
-                    }
-#pragma unroll
-                    for (int k = 0; k < 16; k += 2) add_scaled(sum[c + k], sum[c + k + 1], v[now][k], v[now][k + 1], scale);
-                }
+                if (lane == 0) mbar_arrive(smem_u32(&scales_empty[chunk & 1]));
             }
             if (!ok) {
 #pragma unroll
                 for (int c = 0; c < kPairCols; ++c) sum[c] = __uint_as_float(0x7fffffffu);
             }
-            const float *bias = staged + (chunk & 1) * kScales + kScaleBlocks * kScalePitch + part * kPairCols;
-#pragma unroll
-            for (int c = 0; c < kPairCols; c += 4) {
-                const float4 b = *reinterpret_cast<const float4 *>(bias + c);
-                sum[c] += b.x; sum[c + 1] += b.y; sum[c + 2] += b.z; sum[c + 3] += b.w;
-            }
-            __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&scales_empty[chunk & 1]));
-            ++chunk;
             // a thread has a row, memory wants columns side by side: 32 x 32 words at a time change places within the warp
             const int rows = min(32, p.rows - m0);
 #pragma unroll
