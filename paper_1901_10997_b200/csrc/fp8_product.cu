@@ -498,10 +498,7 @@ fp8_many_rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
                 __syncwarp();
 #pragma unroll
                 for (int w = 0; w < 32; w += 2) {
-                    Vec<T, 2 * kWord> v;
-#pragma unroll
-                    for (int c = 0; c < 2 * kWord; ++c) v.e[c] = T(sum[c0 + w * kWord + c]);
-                    *reinterpret_cast<Vec<T, 2 * kWord> *>(turn + lane * kTurnPitch + w) = v;
+                    *reinterpret_cast<Vec<T, 2 * kWord> *>(turn + lane * kTurnPitch + w) = to_vec<T, 2 * kWord>(&sum[c0 + w * kWord]);
                 }
                 __syncwarp();
                 T *out = y + (long long)m0 * p.y_ld + n0 + c0;

@@ -14,31 +14,34 @@ struct QuantArgs {
     uint8_t *q;
     long long q_ld;
     float *scales;              // [ceil(rows / block rows)][ceil(width / 128)]
+    int strips;                 // of a warp, where a scale belongs to one row
 };
 
-// a warp takes four strips of rows: enough loads in flight, and the strips of one row lie side by side
+// A warp takes up to four neighbouring strips of one row (as many as divide the row evenly), all of them loaded first.
 constexpr int kStripsPerWarp = 4;
 template <typename T, int V>
 __global__ void __launch_bounds__(256) fp8_quantize_rows_kernel(const __grid_constant__ QuantArgs p)
 {
-    const int lane = threadIdx.x & 31;
-    const int strips = (p.width + kStrip - 1) / kStrip, blocks = (p.width + 127) / 128;
-    const long long all = (long long)p.rows * strips, at = ((long long)blockIdx.x * 8 + (threadIdx.x >> 5)) * kStripsPerWarp;
-    float x[kStripsPerWarp][8];
+    const int lane = threadIdx.x & 31, blocks = (p.width + 127) / 128;
+    const long long row = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+    if (row >= p.rows) return;
+    const int first = blockIdx.y * p.strips * kStrip;
+    const T *from = (const T *)p.x + row * p.x_ld;
+    Strip<T, V> raw[kStripsPerWarp];
+#pragma unroll
+    for (int j = 0; j < kStripsPerWarp; ++j)
+        if (j < p.strips) raw[j].load(from, first + j * kStrip, p.width, lane);
 #pragma unroll
     for (int j = 0; j < kStripsPerWarp; ++j) {
-        const long long row = (at + j) / strips;
-        if (at + j < all) load_strip<T, V>((const T *)p.x + row * p.x_ld, (int)(at + j - row * strips) * kStrip, p.width, lane, x[j]);
-    }
+        const int c0 = first + j * kStrip;
+        if (j >= p.strips || c0 >= p.width) break;
+        float x[8];
 #pragma unroll
-    for (int j = 0; j < kStripsPerWarp; ++j) {
-        if (at + j >= all) break;
-        const long long row = (at + j) / strips;
-        const int c0 = (int)(at + j - row * strips) * kStrip;
+        for (int i = 0; i < 8; ++i) x[i] = raw[j][i];
         unsigned top[2];
-        strip_magnitudes<V>(x[j], lane, top);
-        const float s0 = block_scale(top[0]), s1 = block_scale(top[1]);
-        store_strip_e4m3<V>(p.q + row * p.q_ld, c0, p.width, lane, x[j], __fdiv_rn(1.0f, s0), __fdiv_rn(1.0f, s1));
+        strip_magnitudes<V>(x, lane, top);
+        const float s0 = block_scale(top[0]), s1 = V == 8 ? s0 : block_scale(top[1]);
+        store_strip_e4m3<V>(p.q + row * p.q_ld, c0, p.width, lane, x, s0, s1);
         float *out = p.scales + row * blocks + c0 / 128;
         if (lane == 0) out[0] = s0;
         if (lane == 16 && c0 + 128 < p.width) out[1] = s1;
@@ -76,11 +79,10 @@ __global__ void __launch_bounds__(512) fp8_quantize_blocks_kernel(const __grid_c
 #pragma unroll
     for (int i = 0; i < 16; ++i) { top[0] = max(top[0], tops[i][0]); top[1] = max(top[1], tops[i][1]); }
     const float s0 = block_scale(top[0]), s1 = block_scale(top[1]);
-    const float i0 = __fdiv_rn(1.0f, s0), i1 = __fdiv_rn(1.0f, s1);
-    const float mine = V == 8 && lane >= 16 ? i1 : i0;
+    const float mine = V == 8 && lane >= 16 ? s1 : s0;
 #pragma unroll
     for (int j = 0; j < 8; ++j)
-        if (r0 + j < p.rows) store_strip_e4m3<V>(p.q + (r0 + j) * p.q_ld, c0, p.width, lane, x[j], mine, i1);
+        if (r0 + j < p.rows) store_strip_e4m3<V>(p.q + (r0 + j) * p.q_ld, c0, p.width, lane, x[j], mine, s1);
     if (threadIdx.x == 0) {
         float *out = p.scales + (long long)blockIdx.y * blocks + c0 / 128;
         out[0] = s0;
@@ -89,17 +91,18 @@ __global__ void __launch_bounds__(512) fp8_quantize_blocks_kernel(const __grid_c
 }
 
 template <typename T, int V>
-void launch(const QuantArgs &p, int block_rows, cudaStream_t st)
+void launch(QuantArgs &p, int block_rows, cudaStream_t st)
 {
-    const long long strips = (p.width + kStrip - 1) / kStrip;
+    const int strips = (int)((p.width + (long long)kStrip - 1) / kStrip), groups = (strips + kStripsPerWarp - 1) / kStripsPerWarp;
+    p.strips = (strips + groups - 1) / groups;
     if (block_rows == 1)
-        fp8_quantize_rows_kernel<T, V><<<(unsigned)((p.rows * strips + 8 * kStripsPerWarp - 1) / (8 * kStripsPerWarp)), 256, 0, st>>>(p);
+        fp8_quantize_rows_kernel<T, V><<<dim3((unsigned)((p.rows + 7ll) / 8), (unsigned)groups), 256, 0, st>>>(p);
     else
-        fp8_quantize_blocks_kernel<T, V><<<dim3((unsigned)strips, (unsigned)((p.rows + 127) / 128)), 512, 0, st>>>(p);
+        fp8_quantize_blocks_kernel<T, V><<<dim3((unsigned)strips, (unsigned)((p.rows + 127ll) / 128)), 512, 0, st>>>(p);
 }
 
 template <typename T>
-void by_vector(const QuantArgs &p, int v, int block_rows, cudaStream_t st)
+void by_vector(QuantArgs &p, int v, int block_rows, cudaStream_t st)
 {
     if (v == 8) launch<T, 8>(p, block_rows, st);
     else if (v == 4) launch<T, 4>(p, block_rows, st);
@@ -125,12 +128,12 @@ extern "C" int lstm_fp8_quantize(const void *x, long long x_ld, int rows, int wi
     if (!aligned_to(x, es) || !aligned_to(scales, 4)) return fail(LSTM_ERR_INVALID, "bad argument: a pointer is not aligned to its elements");
     if (!aligned_to(q, 16) || q_ld % 16) return fail(LSTM_ERR_INVALID, "bad argument: 8-bit rows must start on 16 bytes");
     if (block_rows == 128 && (rows + 127ll) / 128 > 65535) return fail(LSTM_ERR_UNSUPPORTED, "more than 65535 blocks of rows");
-    if (block_rows == 1 && (rows * ((width + 255ll) / 256) + 31) / 32 > 0x7fffffffll) return fail(LSTM_ERR_UNSUPPORTED, "too many blocks");
+    if (block_rows == 1 && (width + 1023ll) / 1024 > 65535) return fail(LSTM_ERR_UNSUPPORTED, "rows of more than 65535 x 1024 columns");
     int sms = 0;
     if (const int rc = device_sms(sms, fail)) return rc;
     RowAlignment al(width);
     al.matrix(x, x_ld, es);
-    QuantArgs p = {x, x_ld, rows, width, (uint8_t *)q, q_ld, scales};
+    QuantArgs p = {x, x_ld, rows, width, (uint8_t *)q, q_ld, scales, 0};
     if (dtype == LSTM_BF16) by_vector<__nv_bfloat16>(p, al.v, block_rows, (cudaStream_t)cuda_stream);
     else by_vector<float>(p, al.v, block_rows, (cudaStream_t)cuda_stream);
     const cudaError_t e = cudaGetLastError();

@@ -277,10 +277,10 @@ struct Joiner {
 template <typename T, int V, bool GATE>
 __device__ __forceinline__ Vec<T, V> keep()
 {
-    Vec<T, V> r;
+    float o[V];
 #pragma unroll
-    for (int v = 0; v < V; ++v) r.e[v] = T(GATE ? __int_as_float(0x7f800000) : 1.0f);
-    return r;
+    for (int v = 0; v < V; ++v) o[v] = GATE ? __int_as_float(0x7f800000) : 1.0f;
+    return to_vec<T, V>(o);
 }
 
 // ---------------------------------------------------------------------------------------------------

@@ -64,8 +64,13 @@ template <> struct WordOf<4> { typedef unsigned type; };
 template <> struct WordOf<8> { typedef uint2 type; };
 template <> struct WordOf<16> { typedef uint4 type; };
 
+// Kept as the words that were loaded: two bf16 in a register stay one until they are looked at.
 template <typename T, int V>
-struct alignas(sizeof(T) * V <= 16 ? sizeof(T) * V : 16) Vec { T e[V]; };
+struct alignas(sizeof(T) * V <= 16 ? sizeof(T) * V : 16) Vec {
+    static constexpr int kBytes = sizeof(T) * V, kHeld = kBytes < 4 ? 1 : kBytes / 4;
+    typedef typename WordOf<kBytes < 4 ? kBytes : 4>::type Held;
+    Held w[kHeld];
+};
 
 template <typename T, int V>
 __device__ __forceinline__ Vec<T, V> load_vec(const T *p)
@@ -82,23 +87,47 @@ __device__ __forceinline__ Vec<T, V> zero_vec()
 {
     Vec<T, V> v;
 #pragma unroll
-    for (int i = 0; i < V; ++i) v.e[i] = T(0.0f);
+    for (int i = 0; i < Vec<T, V>::kHeld; ++i) v.w[i] = 0;
     return v;
 }
 template <typename T, int V>
-__device__ __forceinline__ float get(const Vec<T, V> &v, int i) { return static_cast<float>(v.e[i]); }
-
+__device__ __forceinline__ float get(const Vec<T, V> &v, int i)
+{
+    if (sizeof(T) == 4) return __uint_as_float(v.w[i]);
+    const unsigned pair = v.w[i / 2];
+    return __uint_as_float(i % 2 ? pair & 0xffff0000u : pair << 16);
+}
+// rounds to nearest, ties to even
 template <typename T, int V>
-__device__ __forceinline__ void store_vec(T *p, const float (&o)[V])
+__device__ __forceinline__ Vec<T, V> to_vec(const float *o)
+{
+    Vec<T, V> v;
+    if (sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i < Vec<T, V>::kHeld; ++i) v.w[i] = __float_as_uint(o[i]);
+    } else if (V == 1) {
+        v.w[0] = __bfloat16_as_ushort(__float2bfloat16_rn(o[0]));
+    } else {
+#pragma unroll
+        for (int i = 0; i + 1 < V; i += 2) {
+            const __nv_bfloat162 pair = __floats2bfloat162_rn(o[i], o[i + 1]);
+            v.w[i / 2] = *reinterpret_cast<const unsigned *>(&pair);
+        }
+    }
+    return v;
+}
+template <typename T, int V>
+__device__ __forceinline__ void store_raw(T *p, const Vec<T, V> &v)
 {
     constexpr int kBytes = sizeof(T) * V, kWord = kBytes <= 16 ? kBytes : 16;
     typedef typename WordOf<kWord>::type W;
     union { Vec<T, V> v; W w[kBytes / kWord]; } u;
-#pragma unroll
-    for (int i = 0; i < V; ++i) u.v.e[i] = T(o[i]);      // rounds to nearest, ties to even
+    u.v = v;
 #pragma unroll
     for (int i = 0; i < kBytes / kWord; ++i) reinterpret_cast<W *>(p)[i] = u.w[i];
 }
+template <typename T, int V>
+__device__ __forceinline__ void store_vec(T *p, const float (&o)[V]) { store_raw<T, V>(p, to_vec<T, V>(o)); }
 
 inline bool known_type(int dtype) { return dtype == LSTM_F32 || dtype == LSTM_BF16; }
 inline int bytes_of(int dtype) { return dtype == LSTM_BF16 ? 2 : 4; }

@@ -51,16 +51,19 @@ __global__ void __launch_bounds__(WARPS == 1 ? 128 : WARPS * 32) rms_norm_kernel
     if (row >= p.rows) return;                          // whole CTAs where warps meet
     const int first = WARPS == 1 ? 0 : warp;
     const T *x = (const T *)p.x + row * p.x_ld, *res = p.residual ? (const T *)p.residual + row * p.residual_ld : nullptr;
-    float r[NS][8], add[NS][8];
+    float r[NS][8];
+    {
+        Strip<T, V> a[NS], b[NS];
 #pragma unroll
-    for (int j = 0; j < NS; ++j) load_strip<T, V>(x, (first + j * WARPS) * kStrip, p.width, lane, r[j]);
-    if (res) {
+        for (int j = 0; j < NS; ++j) a[j].load(x, (first + j * WARPS) * kStrip, p.width, lane);
+        if (res) {
 #pragma unroll
-        for (int j = 0; j < NS; ++j) load_strip<T, V>(res, (first + j * WARPS) * kStrip, p.width, lane, add[j]);
+            for (int j = 0; j < NS; ++j) b[j].load(res, (first + j * WARPS) * kStrip, p.width, lane);
+        }
 #pragma unroll
         for (int j = 0; j < NS; ++j)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) r[j][i] += add[j][i];
+            for (int i = 0; i < 8; ++i) r[j][i] = res ? a[j][i] + b[j][i] : a[j][i];
     }
     float sum = 0.0f;
 #pragma unroll
@@ -85,8 +88,8 @@ __global__ void __launch_bounds__(WARPS == 1 ? 128 : WARPS * 32) rms_norm_kernel
         }
         unsigned top[2];
         strip_magnitudes<V>(y, lane, top);
-        const float s0 = block_scale(top[0]), s1 = block_scale(top[1]);
-        store_strip_e4m3<V>((uint8_t *)p.y + row * p.y_ld, c0, p.width, lane, y, __fdiv_rn(1.0f, s0), __fdiv_rn(1.0f, s1));
+        const float s0 = block_scale(top[0]), s1 = V == 8 ? s0 : block_scale(top[1]);
+        store_strip_e4m3<V>((uint8_t *)p.y + row * p.y_ld, c0, p.width, lane, y, s0, s1);
         const int blocks = (p.width + 127) / 128;
         float *out = p.scales + row * blocks + c0 / 128;
         if (lane == 0) out[0] = s0;
@@ -105,35 +108,58 @@ struct NormBackArgs {
     float *part;                // [CTAs][width] partial sums of dw
 };
 
-// One CTA of WARPS warps walks over rows; a thread keeps its columns of w and of dw from row to row.
-template <typename T, int V, int WARPS, int NS>
-__global__ void __launch_bounds__(WARPS * 32) rms_norm_backward_kernel(const __grid_constant__ NormBackArgs p)
-{
-    __shared__ float2 s[2][WARPS];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    float dw[NS][8];
-#pragma unroll
-    for (int j = 0; j < NS; ++j)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) dw[j][i] = 0.0f;
-    int turn = 0;
-    for (long long row = blockIdx.x; row < p.rows; row += gridDim.x, turn ^= 1) {
-        const T *pr = (const T *)p.r + row * p.r_ld, *py = (const T *)p.dy + row * p.dy_ld;
-        float r[NS][8], dy[NS][8];
+// A CTA walks over rows, NS strips a warp; a thread keeps its columns of dw from row to row.  With one or two strips it keeps those of
+// w too and has the next row's loads under way while it works on one (25600 x 1500 without: 148 us); four leave no registers for it.
+constexpr int kBackWarps = 16;
+template <typename T, int V, int NS, bool DR>
+struct BackRow {
+    Strip<T, V> r[NS], dy[NS], dr[DR ? NS : 1];
+    __device__ __forceinline__ void load(const NormBackArgs &p, long long row, int first, int warps, int lane)
+    {
 #pragma unroll
         for (int j = 0; j < NS; ++j) {
-            load_strip<T, V>(pr, (warp + j * WARPS) * kStrip, p.width, lane, r[j]);
-            load_strip<T, V>(py, (warp + j * WARPS) * kStrip, p.width, lane, dy[j]);
+            const int c0 = (first + j * warps) * kStrip;
+            r[j].load((const T *)p.r + row * p.r_ld, c0, p.width, lane);
+            dy[j].load((const T *)p.dy + row * p.dy_ld, c0, p.width, lane);
+            if (DR && p.dr) dr[DR ? j : 0].load((const T *)p.dr + row * p.dr_ld, c0, p.width, lane);
+        }
+    }
+};
+
+template <typename T, int V, int NS>
+__global__ void __launch_bounds__(NS == 4 ? 512 : 256) rms_norm_backward_kernel(const __grid_constant__ NormBackArgs p)
+{
+    constexpr bool kAhead = NS <= 2;
+    __shared__ float2 s[2][kBackWarps];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    float w[kAhead ? NS : 1][8], dw[NS][8];
+#pragma unroll
+    for (int j = 0; j < NS; ++j) {
+        if (kAhead) load_strip<float, V>(p.w, (warp + j * warps) * kStrip, p.width, lane, w[kAhead ? j : 0]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) dw[j][i] = 0.0f;
+    }
+    typedef BackRow<T, V, NS, kAhead> Row;
+    Row now, next;
+    long long row = blockIdx.x;
+    if (kAhead && row < p.rows) next.load(p, row, warp, warps, lane);
+    const float each = 1.0f / (float)p.width;
+    for (int turn = 0; row < p.rows; row += gridDim.x, turn ^= 1) {
+        if (kAhead) {
+            now = next;
+            if (row + gridDim.x < p.rows) next.load(p, row + gridDim.x, warp, warps, lane);
+        } else {
+            now.load(p, row, warp, warps, lane);
         }
         float rr = 0.0f, ry = 0.0f;
 #pragma unroll
         for (int j = 0; j < NS; ++j) {
-            float w[8];
-            load_strip<float, V>(p.w, (warp + j * WARPS) * kStrip, p.width, lane, w);
+            if (!kAhead) load_strip<float, V>(p.w, (warp + j * warps) * kStrip, p.width, lane, w[0]);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                rr = fmaf(r[j][i], r[j][i], rr);
-                ry = fmaf(r[j][i], w[i] * dy[j][i], ry);
+                const float r = now.r[j][i];
+                rr = fmaf(r, r, rr);
+                ry = fmaf(r, w[kAhead ? j : 0][i] * now.dy[j][i], ry);
             }
         }
 #pragma unroll
@@ -141,33 +167,35 @@ __global__ void __launch_bounds__(WARPS * 32) rms_norm_backward_kernel(const __g
             rr += __shfl_xor_sync(0xffffffffu, rr, o);
             ry += __shfl_xor_sync(0xffffffffu, ry, o);
         }
-        if (lane == 0) s[turn][warp] = make_float2(rr, ry);
-        __syncthreads();                                // the other set is read no more once all have come here
-        rr = ry = 0.0f;
-#pragma unroll
-        for (int i = 0; i < WARPS; ++i) { rr += s[turn][i].x; ry += s[turn][i].y; }
-        const float rstd = 1.0f / sqrtf(rr / (float)p.width + p.eps);
-        const float mean = ry / (float)p.width * rstd * rstd;
+        if (warps > 1) {
+            if (lane == 0) s[turn][warp] = make_float2(rr, ry);
+            __syncthreads();                            // the other set is read no more once all have come here
+            rr = ry = 0.0f;
+            for (int i = 0; i < warps; ++i) { rr += s[turn][i].x; ry += s[turn][i].y; }
+        }
+        const float rstd = 1.0f / sqrtf(rr * each + p.eps);
+        const float mean = ry * each * rstd * rstd;
 #pragma unroll
         for (int j = 0; j < NS; ++j) {
-            const int c0 = (warp + j * WARPS) * kStrip;
-            if (c0 >= p.width) break;
-            float w[8], o[8];
-            load_strip<float, V>(p.w, c0, p.width, lane, w);
-            float past[8];
-            if (p.dr) load_strip<T, V>((const T *)p.dr + row * p.dr_ld, c0, p.width, lane, past);
+            const int c0 = (warp + j * warps) * kStrip;
+            if (!kAhead) {
+                load_strip<float, V>(p.w, c0, p.width, lane, w[0]);
+                if (p.dr) now.dr[0].load((const T *)p.dr + row * p.dr_ld, c0, p.width, lane);
+            }
+            float o[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                dw[j][i] = fmaf(dy[j][i], r[j][i] * rstd, dw[j][i]);
-                o[i] = rstd * (w[i] * dy[j][i] - r[j][i] * mean);
-                if (p.dr) o[i] += past[i];
+                const float r = now.r[j][i], dy = now.dy[j][i];
+                dw[j][i] = fmaf(dy, r * rstd, dw[j][i]);
+                o[i] = rstd * (w[kAhead ? j : 0][i] * dy - r * mean);
+                if (p.dr) o[i] += now.dr[kAhead ? j : 0][i];
             }
             store_strip<T, V>((T *)p.dx + row * p.dx_ld, c0, p.width, lane, o);
         }
     }
 #pragma unroll
     for (int j = 0; j < NS; ++j)
-        store_strip<float, V>(p.part + (long long)blockIdx.x * p.width, (warp + j * WARPS) * kStrip, p.width, lane, dw[j]);
+        store_strip<float, V>(p.part + (long long)blockIdx.x * p.width, (warp + j * warps) * kStrip, p.width, lane, dw[j]);
 }
 
 // dw = sum of the CTAs' rows, always in the same order: 32 columns a CTA, thread (column, i) adds rows i, i + 32, ...
@@ -199,20 +227,30 @@ void launch_norm(const NormArgs &p, cudaStream_t st)
     else rms_norm_kernel<T, V, 8, 8><<<p.rows, 256, 0, st>>>(p);
 }
 
+// strips of a warp and warps of a CTA for a width: few strips a warp, and no idle one but in the last
+struct BackShape {
+    int ns, warps;
+    explicit BackShape(int width)
+    {
+        const int strips = (width + kStrip - 1) / kStrip;
+        ns = strips <= 2 ? 1 : strips <= 16 ? 2 : 4;
+        warps = (strips + ns - 1) / ns;
+    }
+};
 template <typename T, int V>
 void launch_back(const NormBackArgs &p, int parts, cudaStream_t st)
 {
-    if (p.width <= 1024) rms_norm_backward_kernel<T, V, 4, 1><<<parts, 128, 0, st>>>(p);
-    else if (p.width <= 2048) rms_norm_backward_kernel<T, V, 4, 2><<<parts, 128, 0, st>>>(p);
-    else if (p.width <= 4096) rms_norm_backward_kernel<T, V, 4, 4><<<parts, 128, 0, st>>>(p);
-    else if (p.width <= 8192) rms_norm_backward_kernel<T, V, 8, 4><<<parts, 256, 0, st>>>(p);
-    else rms_norm_backward_kernel<T, V, 16, 4><<<parts, 512, 0, st>>>(p);
+    const BackShape s(p.width);
+    if (s.ns == 1) rms_norm_backward_kernel<T, V, 1><<<parts, s.warps * 32, 0, st>>>(p);
+    else if (s.ns == 2) rms_norm_backward_kernel<T, V, 2><<<parts, s.warps * 32, 0, st>>>(p);
+    else rms_norm_backward_kernel<T, V, 4><<<parts, s.warps * 32, 0, st>>>(p);
 }
 
-// CTAs of the backward kernel, each of which leaves a row of partial sums
+// CTAs of the backward kernel, each of which leaves a row of partial sums: 16 warps an SM
 int parts_of(int rows, int width, int sms)
 {
-    const int resident = width <= 4096 ? 6 : width <= 8192 ? 2 : 1;
+    const BackShape s(width);
+    const int resident = s.warps >= 16 ? 1 : 16 / s.warps;
     return rows < sms * resident ? rows : sms * resident;
 }
 

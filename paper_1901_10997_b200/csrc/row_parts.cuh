@@ -26,6 +26,20 @@ __device__ __forceinline__ void load_strip(const T *row, int c0, int width, int 
         for (int i = 0; i < V; ++i) o[q * V + i] = get<T, V>(v, i);
     }
 }
+// ... as they lie in memory, so that a row's loads can all be under way before the first is looked at
+template <typename T, int V>
+struct Strip {
+    Vec<T, V> v[8 / V];
+    __device__ __forceinline__ void load(const T *row, int c0, int width, int lane)
+    {
+#pragma unroll
+        for (int q = 0; q < 8 / V; ++q) {
+            const int c = c0 + strip_col<V>(q, lane);
+            v[q] = c < width ? load_vec<T, V>(row + c) : zero_vec<T, V>();
+        }
+    }
+    __device__ __forceinline__ float operator[](int i) const { return get<T, V>(v[i / V], i % V); }
+};
 template <typename T, int V>
 __device__ __forceinline__ void store_strip(T *row, int c0, int width, int lane, const float (&o)[8])
 {
@@ -49,7 +63,21 @@ __device__ __forceinline__ float block_scale(unsigned largest)
     const unsigned least = 0x04e00000u;                 // 448 * 2^-126
     return __fdiv_rn(__uint_as_float(max(largest, least)), kE4m3Max);
 }
-// four values as e4m3, the nearest, at most 448 in magnitude
+// What an element is multiplied by to be in units of the scale.  The product's remainder corrects it (`in_units`), so that what is
+// rounded to e4m3 is the quotient as fp32 has it: without that one value in some ten thousand lands on the other side of a tie.
+__device__ __forceinline__ float per_scale(float scale)
+{
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(scale));
+    return y;
+}
+// (scale: at most the largest finite number; beside an infinite one, finite values are zero)
+__device__ __forceinline__ float in_units(float x, float scale, float per)
+{
+    const float t = x * per;
+    return fmaf(fmaf(-t, scale, x), per, t);
+}
+// two values as e4m3, the nearest, at most 448 in magnitude
 __device__ __forceinline__ unsigned to_e4m3x2(float a, float b)
 {
     return __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
@@ -79,25 +107,28 @@ __device__ __forceinline__ void strip_magnitudes(const float (&y)[8], int lane, 
 
 // the lane's 8 elements, divided by their blocks' scales, as e4m3 bytes
 template <int V>
-__device__ __forceinline__ void store_strip_e4m3(uint8_t *row, int c0, int width, int lane, const float (&y)[8], float inv0, float inv1)
+__device__ __forceinline__ void store_strip_e4m3(uint8_t *row, int c0, int width, int lane, const float (&x)[8], float s0, float s1)
 {
+    const float per0 = per_scale(s0), per1 = V == 8 ? per0 : per_scale(s1);
+    const float f0 = fminf(s0, 3.4028235e38f), f1 = fminf(s1, 3.4028235e38f);
+    float y[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = V == 8 || i < 4 ? in_units(x[i], f0, per0) : in_units(x[i], f1, per1);
 #pragma unroll
     for (int q = 0; q < 8 / V; ++q) {
         const int c = c0 + strip_col<V>(q, lane);
         if (c >= width) continue;
-        const float inv = V == 8 ? inv0 : q * V < 4 ? inv0 : inv1;
         unsigned w[V == 8 ? 2 : 1];
         if (V == 1) {
-            w[0] = to_e4m3x2(y[q] * inv, 0.0f);
+            w[0] = to_e4m3x2(y[q], 0.0f);
             row[c] = (uint8_t)w[0];
         } else if (V == 2) {
-            w[0] = to_e4m3x2(y[2 * q] * inv, y[2 * q + 1] * inv);
+            w[0] = to_e4m3x2(y[2 * q], y[2 * q + 1]);
             *reinterpret_cast<unsigned short *>(row + c) = (unsigned short)w[0];
         } else {
 #pragma unroll
             for (int i = 0; i < V / 4; ++i)
-                w[i] = to_e4m3x2(y[q * V + 4 * i] * inv, y[q * V + 4 * i + 1] * inv) |
-                       to_e4m3x2(y[q * V + 4 * i + 2] * inv, y[q * V + 4 * i + 3] * inv) << 16;
+                w[i] = to_e4m3x2(y[q * V + 4 * i], y[q * V + 4 * i + 1]) | to_e4m3x2(y[q * V + 4 * i + 2], y[q * V + 4 * i + 3]) << 16;
             if (V == 4) *reinterpret_cast<unsigned *>(row + c) = w[0];
             if (V == 8) *reinterpret_cast<uint2 *>(row + c) = make_uint2(w[0], w[V == 8 ? 1 : 0]);
         }
