@@ -4,8 +4,8 @@
 //
 // and its gradients  dx = rstd (w dy - r rstd^2 mean(w dy r)) + dr,   dw = sum over rows of dy r rstd.
 //
-// Bound by memory: a row is read once into the registers of one warp (up to 2048 columns) or of 4 or 8 warps, summed by shuffles,
-// and written once.  Sums are fp32 over at most 64 elements a lane before they are joined pairwise.
+// Bound by memory: a row is read once into the registers of one warp (up to 512 columns) or of up to 16, summed by shuffles, and
+// written once.  Sums are fp32 over at most 32 elements a lane before they are joined pairwise.
 #include "../../include/lstm_b200.h"
 #include "row_parts.cuh"
 
@@ -25,56 +25,55 @@ struct NormArgs {
     long long r_ld;
 };
 
-// sum over the WARPS warps that share a row; s holds two sets, used in turn
-template <int WARPS>
-__device__ __forceinline__ float row_sum(float v, float *s)
+// NS strips a warp.  Up to two strips, a warp has a row to itself and four stand in a CTA; wider rows have a CTA each, whose
+// warps meet once.  Few registers a thread and many CTAs: that, not the work of a thread, is what keeps the memory busy.
+constexpr int kNormWarps = 16;
+template <typename T, int V, int NS, bool ALONE>
+__global__ void __launch_bounds__(ALONE ? 128 : NS == 2 ? 256 : 512, ALONE ? 12 : NS == 2 ? 4 : 1) rms_norm_kernel(const __grid_constant__ NormArgs p)
 {
-#pragma unroll
-    for (int o = 16; o > 0; o /= 2) v += __shfl_xor_sync(0xffffffffu, v, o);
-    if (WARPS == 1) return v;
+    __shared__ float s[kNormWarps];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    if (lane == 0) s[warp] = v;
-    __syncthreads();
-    v = 0.0f;
-#pragma unroll
-    for (int i = 0; i < WARPS; ++i) v += s[i];
-    return v;
-}
-
-// WARPS warps a row, NS strips a warp; rows of one warp stand four to a CTA
-template <typename T, int V, int WARPS, int NS>
-__global__ void __launch_bounds__(WARPS == 1 ? 128 : WARPS * 32) rms_norm_kernel(const __grid_constant__ NormArgs p)
-{
-    __shared__ float s[WARPS];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const long long row = WARPS == 1 ? (long long)blockIdx.x * 4 + warp : blockIdx.x;
-    if (row >= p.rows) return;                          // whole CTAs where warps meet
-    const int first = WARPS == 1 ? 0 : warp;
+    const int first = ALONE ? 0 : warp, warps = ALONE ? 1 : blockDim.x >> 5;
+    const long long row = ALONE ? (long long)blockIdx.x * 4 + warp : blockIdx.x;
+    if (row >= p.rows) return;                          // whole warps where they do not meet
     const T *x = (const T *)p.x + row * p.x_ld, *res = p.residual ? (const T *)p.residual + row * p.residual_ld : nullptr;
     float r[NS][8];
     {
         Strip<T, V> a[NS], b[NS];
 #pragma unroll
-        for (int j = 0; j < NS; ++j) a[j].load(x, (first + j * WARPS) * kStrip, p.width, lane);
+        for (int j = 0; j < NS; ++j) a[j].load(x, (first + j * warps) * kStrip, p.width, lane);
         if (res) {
 #pragma unroll
-            for (int j = 0; j < NS; ++j) b[j].load(res, (first + j * WARPS) * kStrip, p.width, lane);
+            for (int j = 0; j < NS; ++j) b[j].load(res, (first + j * warps) * kStrip, p.width, lane);
         }
 #pragma unroll
         for (int j = 0; j < NS; ++j)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) r[j][i] = res ? a[j][i] + b[j][i] : a[j][i];
+            for (int i = 0; i < 8; ++i) r[j][i] = a[j][i];
+        if (res) {
+#pragma unroll
+            for (int j = 0; j < NS; ++j)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) r[j][i] += b[j][i];
+        }
     }
     float sum = 0.0f;
 #pragma unroll
     for (int j = 0; j < NS; ++j)
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum = fmaf(r[j][i], r[j][i], sum);
-    sum = row_sum<WARPS>(sum, s);
-    const float rstd = 1.0f / sqrtf(sum / (float)p.width + p.eps);
+#pragma unroll
+    for (int o = 16; o > 0; o /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (!ALONE) {
+        if (lane == 0) s[warp] = sum;
+        __syncthreads();
+        sum = 0.0f;
+        for (int i = 0; i < warps; ++i) sum += s[i];
+    }
+    const float rstd = rsqrtf(sum / (float)p.width + p.eps);
 #pragma unroll
     for (int j = 0; j < NS; ++j) {
-        const int c0 = (first + j * WARPS) * kStrip;
+        const int c0 = (first + j * warps) * kStrip;
         if (c0 >= p.width) break;
         // the norm continues from the sum as it is, not from the rounded copy that is handed on: one rounding an output
         if (p.r) store_strip<T, V>((T *)p.r + row * p.r_ld, c0, p.width, lane, r[j]);
@@ -173,7 +172,7 @@ __global__ void __launch_bounds__(NS == 4 ? 512 : 256) rms_norm_backward_kernel(
             rr = ry = 0.0f;
             for (int i = 0; i < warps; ++i) { rr += s[turn][i].x; ry += s[turn][i].y; }
         }
-        const float rstd = 1.0f / sqrtf(rr * each + p.eps);
+        const float rstd = rsqrtf(rr * each + p.eps);
         const float mean = ry * each * rstd * rstd;
 #pragma unroll
         for (int j = 0; j < NS; ++j) {
@@ -217,39 +216,37 @@ __global__ void __launch_bounds__(1024) rms_norm_join_kernel(const float *part, 
     if (threadIdx.x == 0 && col < width) dw[col] = v;
 }
 
-template <typename T, int V>
-void launch_norm(const NormArgs &p, cudaStream_t st)
-{
-    // one warp a row as far as its registers go (64 elements a lane), then 4 and 8 warps
-    if (p.width <= 512) rms_norm_kernel<T, V, 1, 2><<<(unsigned)((p.rows + 3ll) / 4), 128, 0, st>>>(p);
-    else if (p.width <= 2048) rms_norm_kernel<T, V, 1, 8><<<(unsigned)((p.rows + 3ll) / 4), 128, 0, st>>>(p);
-    else if (p.width <= 8192) rms_norm_kernel<T, V, 4, 8><<<p.rows, 128, 0, st>>>(p);
-    else rms_norm_kernel<T, V, 8, 8><<<p.rows, 256, 0, st>>>(p);
-}
-
 // strips of a warp and warps of a CTA for a width: few strips a warp, and no idle one but in the last
-struct BackShape {
+struct RowShape {
     int ns, warps;
-    explicit BackShape(int width)
+    explicit RowShape(int width)
     {
         const int strips = (width + kStrip - 1) / kStrip;
-        ns = strips <= 2 ? 1 : strips <= 16 ? 2 : 4;
+        ns = strips <= 16 ? 2 : 4;
         warps = (strips + ns - 1) / ns;
     }
 };
 template <typename T, int V>
+void launch_norm(const NormArgs &p, cudaStream_t st)
+{
+    const RowShape s(p.width);
+    if (s.warps == 1) rms_norm_kernel<T, V, 2, true><<<(unsigned)((p.rows + 3ll) / 4), 128, 0, st>>>(p);
+    else if (s.ns == 2) rms_norm_kernel<T, V, 2, false><<<p.rows, s.warps * 32, 0, st>>>(p);
+    else rms_norm_kernel<T, V, 4, false><<<p.rows, s.warps * 32, 0, st>>>(p);
+}
+
+template <typename T, int V>
 void launch_back(const NormBackArgs &p, int parts, cudaStream_t st)
 {
-    const BackShape s(p.width);
-    if (s.ns == 1) rms_norm_backward_kernel<T, V, 1><<<parts, s.warps * 32, 0, st>>>(p);
-    else if (s.ns == 2) rms_norm_backward_kernel<T, V, 2><<<parts, s.warps * 32, 0, st>>>(p);
+    const RowShape s(p.width);
+    if (s.ns == 2) rms_norm_backward_kernel<T, V, 2><<<parts, s.warps * 32, 0, st>>>(p);
     else rms_norm_backward_kernel<T, V, 4><<<parts, s.warps * 32, 0, st>>>(p);
 }
 
 // CTAs of the backward kernel, each of which leaves a row of partial sums: 16 warps an SM
 int parts_of(int rows, int width, int sms)
 {
-    const BackShape s(width);
+    const RowShape s(width);
     const int resident = s.warps >= 16 ? 1 : 16 / s.warps;
     return rows < sms * resident ? rows : sms * resident;
 }

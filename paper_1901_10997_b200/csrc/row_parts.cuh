@@ -61,7 +61,9 @@ __device__ __forceinline__ unsigned magnitude(float x) { return __float_as_uint(
 __device__ __forceinline__ float block_scale(unsigned largest)
 {
     const unsigned least = 0x04e00000u;                 // 448 * 2^-126
-    return __fdiv_rn(__uint_as_float(max(largest, least)), kE4m3Max);
+    const float top = __uint_as_float(max(largest, least)), t = top * (1.0f / kE4m3Max);
+    const float s = fmaf(fmaf(-t, kE4m3Max, top), 1.0f / kE4m3Max, t);       // corrected by its remainder
+    return largest < 0x7f800000u ? s : top;
 }
 // What an element is multiplied by to be in units of the scale.  The product's remainder corrects it (`in_units`), so that what is
 // rounded to e4m3 is the quotient as fp32 has it: without that one value in some ten thousand lands on the other side of a tie.
