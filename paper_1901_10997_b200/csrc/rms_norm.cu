@@ -235,20 +235,32 @@ void launch_norm(const NormArgs &p, cudaStream_t st)
     else rms_norm_kernel<T, V, 4, false><<<p.rows, s.warps * 32, 0, st>>>(p);
 }
 
-template <typename T, int V>
-void launch_back(const NormBackArgs &p, int parts, cudaStream_t st)
-{
-    const RowShape s(p.width);
-    if (s.ns == 2) rms_norm_backward_kernel<T, V, 2><<<parts, s.warps * 32, 0, st>>>(p);
-    else rms_norm_backward_kernel<T, V, 4><<<parts, s.warps * 32, 0, st>>>(p);
-}
-
-// CTAs of the backward kernel, each of which leaves a row of partial sums: 16 warps an SM
+// the most CTAs of the backward kernel, each of which leaves a row of partial sums: 16 warps an SM
 int parts_of(int rows, int width, int sms)
 {
     const RowShape s(width);
     const int resident = s.warps >= 16 ? 1 : 16 / s.warps;
     return rows < sms * resident ? rows : sms * resident;
+}
+// ... of which as many are launched as are resident at once; returns how many
+template <typename T, int V, int NS>
+int launch_back_shape(const NormBackArgs &p, int warps, int parts, int sms, cudaStream_t st)
+{
+    static std::atomic<int> resident[kBackWarps + 1];
+    int n = resident[warps].load(std::memory_order_relaxed);
+    if (n == 0) {
+        if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, rms_norm_backward_kernel<T, V, NS>, warps * 32, 0) != cudaSuccess || n < 1) n = 1;
+        resident[warps].store(n, std::memory_order_relaxed);
+    }
+    if (parts > n * sms) parts = n * sms;
+    rms_norm_backward_kernel<T, V, NS><<<parts, warps * 32, 0, st>>>(p);
+    return parts;
+}
+template <typename T, int V>
+int launch_back(const NormBackArgs &p, int parts, int sms, cudaStream_t st)
+{
+    const RowShape s(p.width);
+    return s.ns == 2 ? launch_back_shape<T, V, 2>(p, s.warps, parts, sms, st) : launch_back_shape<T, V, 4>(p, s.warps, parts, sms, st);
 }
 
 template <template <typename, int> class F, typename... A>
@@ -261,7 +273,7 @@ void by_type(int dtype, int v, A &&...a)
     else half ? F<__nv_bfloat16, 1>::go(a...) : F<float, 1>::go(a...);
 }
 template <typename T, int V> struct Forward { static void go(const NormArgs &p, cudaStream_t st) { launch_norm<T, V>(p, st); } };
-template <typename T, int V> struct Backward { static void go(const NormBackArgs &p, int parts, cudaStream_t st) { launch_back<T, V>(p, parts, st); } };
+template <typename T, int V> struct Backward { static void go(const NormBackArgs &p, int &parts, int sms, cudaStream_t st) { parts = launch_back<T, V>(p, parts, sms, st); } };
 
 int check(int rows, int width, int dtype, float eps, const Failure &fail)
 {
@@ -320,7 +332,7 @@ int lstm_rms_norm_backward(const void *dy, long long dy_ld, const void *r, long 
     int sms = 0;
     if (const int rc = device_sms(sms, fail)) return rc;
     const cudaStream_t st = (cudaStream_t)cuda_stream;
-    const int parts = parts_of(rows, width, sms);
+    int parts = parts_of(rows, width, sms);
     if (parts > 0 && (!workspace || workspace_floats < (long long)parts * width))
         return fail(LSTM_ERR_INVALID, "bad argument: the workspace is smaller than lstm_rms_norm_workspace says");
     if (parts > 0) {
@@ -332,7 +344,7 @@ int lstm_rms_norm_backward(const void *dy, long long dy_ld, const void *r, long 
         al.matrix(w, 0, 4);
         al.matrix(workspace, 0, 4);
         NormBackArgs p = {dy, r, dr, dy_ld, r_ld, dr_ld, w, eps, rows, width, dx, dx_ld, workspace};
-        by_type<Backward>(dtype, al.v, p, parts, st);
+        by_type<Backward>(dtype, al.v, p, parts, sms, st);
     }
     rms_norm_join_kernel<<<(width + 31) / 32, dim3(32, 32), 0, st>>>(workspace, parts, width, dw);
     const cudaError_t e = cudaGetLastError();

@@ -15,41 +15,43 @@ template <int V>
 __device__ __forceinline__ int strip_col(int q, int lane) { return q * 32 * V + lane * V; }
 
 // lane's 8 elements of the strip at column c0; columns behind `width` read as zero
-template <typename T, int V>
-__device__ __forceinline__ void load_strip(const T *row, int c0, int width, int lane, float (&o)[8])
-{
-#pragma unroll
-    for (int q = 0; q < 8 / V; ++q) {
-        const int c = c0 + strip_col<V>(q, lane);
-        const Vec<T, V> v = c < width ? load_vec<T, V>(row + c) : zero_vec<T, V>();
-#pragma unroll
-        for (int i = 0; i < V; ++i) o[q * V + i] = get<T, V>(v, i);
-    }
-}
-// ... as they lie in memory, so that a row's loads can all be under way before the first is looked at
+// (whole strips without a question for each vector: their addresses are one register and constants)
+// as they lie in memory, so that a row's loads can all be under way before the first is looked at
 template <typename T, int V>
 struct Strip {
     Vec<T, V> v[8 / V];
     __device__ __forceinline__ void load(const T *row, int c0, int width, int lane)
     {
+        const T *at = row + c0 + lane * V;
+        if (c0 + kStrip <= width) {
 #pragma unroll
-        for (int q = 0; q < 8 / V; ++q) {
-            const int c = c0 + strip_col<V>(q, lane);
-            v[q] = c < width ? load_vec<T, V>(row + c) : zero_vec<T, V>();
+            for (int q = 0; q < 8 / V; ++q) v[q] = load_vec<T, V>(at + q * 32 * V);
+        } else {
+#pragma unroll
+            for (int q = 0; q < 8 / V; ++q) v[q] = c0 + strip_col<V>(q, lane) < width ? load_vec<T, V>(at + q * 32 * V) : zero_vec<T, V>();
         }
     }
     __device__ __forceinline__ float operator[](int i) const { return get<T, V>(v[i / V], i % V); }
 };
 template <typename T, int V>
+__device__ __forceinline__ void load_strip(const T *row, int c0, int width, int lane, float (&o)[8])
+{
+    Strip<T, V> s;
+    s.load(row, c0, width, lane);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[i] = s[i];
+}
+template <typename T, int V>
 __device__ __forceinline__ void store_strip(T *row, int c0, int width, int lane, const float (&o)[8])
 {
+    T *at = row + c0 + lane * V;
+    if (c0 + kStrip <= width) {
 #pragma unroll
-    for (int q = 0; q < 8 / V; ++q) {
-        const int c = c0 + strip_col<V>(q, lane);
-        float e[V];
+        for (int q = 0; q < 8 / V; ++q) store_raw<T, V>(at + q * 32 * V, to_vec<T, V>(&o[q * V]));
+    } else {
 #pragma unroll
-        for (int i = 0; i < V; ++i) e[i] = o[q * V + i];
-        if (c < width) store_vec<T, V>(row + c, e);
+        for (int q = 0; q < 8 / V; ++q)
+            if (c0 + strip_col<V>(q, lane) < width) store_raw<T, V>(at + q * 32 * V, to_vec<T, V>(&o[q * V]));
     }
 }
 
@@ -112,6 +114,7 @@ template <int V>
 __device__ __forceinline__ void store_strip_e4m3(uint8_t *row, int c0, int width, int lane, const float (&x)[8], float s0, float s1)
 {
     const float per0 = per_scale(s0), per1 = V == 8 ? per0 : per_scale(s1);
+    const bool whole = c0 + kStrip <= width;
     const float f0 = fminf(s0, 3.4028235e38f), f1 = fminf(s1, 3.4028235e38f);
     float y[8];
 #pragma unroll
@@ -119,7 +122,7 @@ __device__ __forceinline__ void store_strip_e4m3(uint8_t *row, int c0, int width
 #pragma unroll
     for (int q = 0; q < 8 / V; ++q) {
         const int c = c0 + strip_col<V>(q, lane);
-        if (c >= width) continue;
+        if (!whole && c >= width) continue;
         unsigned w[V == 8 ? 2 : 1];
         if (V == 1) {
             w[0] = to_e4m3x2(y[q], 0.0f);
