@@ -1,0 +1,326 @@
+// The gated linear recurrence for many channels: a CTA has 32 vectors of channels side by side (whole lines of memory) and walks over
+// time alone; its warps hold consecutive spans of a few steps.  Spans become maps h -> A h + H (see linrec.cu), every warp leaves
+// its own in shared memory, one thread per channel runs through them with the channel's carry and leaves each warp the state in front
+// of its span.  Two barriers a round and about 1.5 instructions an element for the joining; few registers, so that enough warps
+// are resident to keep the memory busy, which is what bounds it: 2048 x 32 x 1500 of bf16 takes 109 us, 0.82 of the copy rate
+// (the kernels of linrec.cu, which can spread one sequence over a cluster, 165).
+//
+// Backward: a round's spans begin at saved states, so the same pass over the maps gives the states in front of the spans (from the
+// saved ones, forwards) and the gradients that arrive behind them (from the carry, backwards).
+#include "../../include/lstm_b200.h"
+#include "linrec_parts.cuh"
+
+#include <type_traits>
+
+namespace lstm {
+namespace {
+
+// Steps of a warp's span, threads of a CTA, CTAs of an SM, and where inputs wait, for vectors of V channels.
+// Vectors of four lie in shared memory two spans ahead (of bf16 in registers: 2048 x 32 x 1500 151 us instead of 109); narrower ones wait
+// in registers (4096 x 8 x 1502 of fp32 in shared memory: 173 us instead of 113).
+template <typename T, int V, bool BACK> struct Shape;
+template <typename T> struct Shape<T, 4, false> { static constexpr int kSteps = 4, kThreads = 128, kResident = 5, kDepth = 2; };
+template <typename T> struct Shape<T, 2, false> { static constexpr int kSteps = 8, kThreads = 256, kResident = 2, kDepth = 0; };
+template <typename T> struct Shape<T, 1, false> { static constexpr int kSteps = 16, kThreads = 128, kResident = 4, kDepth = 0; };
+template <typename T> struct Shape<T, 4, true> { static constexpr int kSteps = 4, kThreads = 128, kResident = 4, kDepth = sizeof(T) == 2 ? 2 : 1; };
+template <typename T> struct Shape<T, 2, true> { static constexpr int kSteps = 4, kThreads = 256, kResident = 2, kDepth = 0; };
+template <typename T> struct Shape<T, 1, true> { static constexpr int kSteps = 8, kThreads = 128, kResident = 4, kDepth = 0; };
+
+template <typename T, int V, int N, bool GATE, bool BACK, typename S = Shape<T, V, BACK>>
+using Inputs = std::conditional_t<S::kDepth == 0, InRegisters<T, V, N, GATE, S::kSteps>, InShared<T, V, N, GATE, S::kSteps, S::kThreads, S::kDepth ? S::kDepth : 1>>;
+
+// a lane's channels, and the one channel whose carry a thread keeps
+template <int V>
+struct Channels {
+    int b, d, len, end;         // steps of the sequence; of the batch (0 where there is no such channel)
+    long long bd, BD, own;      // own: [B][D] index of channel threadIdx.x of the CTA, or -1
+    bool live;
+    __device__ explicit Channels(const LinrecArgs &p)
+    {
+        const long long all = (long long)p.B * p.nvec, vec = (long long)blockIdx.x * 32 + (threadIdx.x & 31);
+        live = vec < all;
+        b = live ? (int)(vec / p.nvec) : 0;
+        d = live ? (int)(vec % p.nvec) * V : 0;
+        len = !live ? 0 : p.lengths ? min(max(p.lengths[b], 0), p.T) : p.T;
+        end = live ? p.T : 0;
+        bd = (long long)b * p.D + d;
+        BD = (long long)p.B * p.D;
+        const long long mine = (long long)blockIdx.x * 32 + threadIdx.x / V;
+        own = threadIdx.x < 32 * V && mine < all ? mine / p.nvec * p.D + mine % p.nvec * V + threadIdx.x % V : -1;
+    }
+};
+
+template <typename T, int V, bool GATE>
+__global__ void __launch_bounds__(Shape<T, V, false>::kThreads, Shape<T, V, false>::kResident) linrec_wide_forward_kernel(const __grid_constant__ LinrecArgs p)
+{
+    typedef Shape<T, V, false> S;
+    constexpr int kSteps = S::kSteps, kWarps = S::kThreads / 32, kSpan = kWarps * kSteps, kC = 32 * V;
+    extern __shared__ __align__(16) unsigned char smem[];
+    __shared__ __align__(16) float mapA[kWarps][kC], mapH[kWarps][kC], front[kWarps][kC];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const Channels<V> at(p);
+    float carry = at.own >= 0 && p.h0 ? p.h0[at.own] : 0.0f;
+    const long long sign = p.reverse ? -1 : 1;
+    const long long step[2] = {sign * p.a_t, sign * p.x_t}, jump[2] = {kSpan * step[0], kSpan * step[1]}, out_step = sign * p.h_t, out_jump = kSpan * out_step;
+    long long i0 = warp * kSteps, ahead = i0;
+    const long long first = p.reverse ? at.len - 1 - i0 : i0;
+    const T *from[2] = {(const T *)p.a + at.b * p.a_b + at.d + first * p.a_t, (const T *)p.x + at.b * p.x_b + at.d + first * p.x_t};
+    T *ph = (T *)p.h + at.b * p.h_b + at.d, *out = ph + first * p.h_t;
+    typedef Inputs<T, V, 2, GATE, false> In;
+    In in(smem);
+    auto fetch = [&]() {
+        in.fetch(from, step, count_steps<kSteps>(ahead, at.len));
+        ahead += kSpan;
+        from[0] += jump[0];
+        from[1] += jump[1];
+    };
+#pragma unroll
+    for (int i = 0; i < In::kDepth; ++i) fetch();
+    for (long long base = 0; base < p.T; base += kSpan, i0 += kSpan, out += out_jump) {
+        const int n = count_steps<kSteps>(i0, at.len);
+        in.next_if_registers();
+        fetch();
+        in.arrived();
+        float f[kSteps][V], add[kSteps][V];
+#pragma unroll
+        for (int k = 0; k < kSteps; ++k) {
+            const Vec<T, V> ra = in.get_vec(0, k), rx = in.get_vec(1, k);
+#pragma unroll
+            for (int v = 0; v < V; ++v) { f[k][v] = get<T, V>(ra, v); add[k][v] = get<T, V>(rx, v); }
+            if (GATE) {
+                float w[V];
+                gate_vec<T, V>(f[k], f[k], w);
+                mul_vec<V>(add[k], add[k], w);
+            }
+        }
+        in.next();
+        float A[V], H[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) { A[v] = f[0][v]; H[v] = add[0][v]; }
+#pragma unroll
+        for (int k = 1; k < kSteps; ++k) {
+            fma_vec<V>(H, f[k], H, add[k]);
+            mul_vec<V>(A, A, f[k]);
+        }
+#pragma unroll
+        for (int v = 0; v < V; ++v) A[v] = held<V, GATE>(A[v]);
+        store_vec<float, V>(&mapA[warp][lane * V], A);
+        store_vec<float, V>(&mapH[warp][lane * V], H);
+        __syncthreads();
+        if (threadIdx.x < kC) {
+            float a[kWarps], h[kWarps];
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) { a[w] = mapA[w][threadIdx.x]; h[w] = mapH[w][threadIdx.x]; }
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) {
+                front[w][threadIdx.x] = carry;
+                carry = fmaf(a[w], carry, h[w]);
+            }
+        }
+        __syncthreads();            // maps are written again behind the next round's first barrier, by when `front` has been read
+        const Vec<float, V> begin = load_vec<float, V>(&front[warp][lane * V]);
+        float h[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) h[v] = get<float, V>(begin, v);
+        if (p.states && i0 < at.end && i0 % LSTM_LINREC_SEGMENT == 0)
+            store_vec<float, V>(p.states + i0 / LSTM_LINREC_SEGMENT * at.BD + at.bd, h);
+        if (n == kSteps) {
+            T *q = out;
+#pragma unroll
+            for (int k = 0; k < kSteps; ++k) {
+                fma_vec<V>(h, f[k], h, add[k]);
+                store_vec<T, V>(q, h);
+                q += out_step;
+            }
+        } else {
+            // steps behind a sequence's end lie at their own place in either direction
+            const int rows = count_steps<kSteps>(i0, at.end);
+#pragma unroll
+            for (int k = 0; k < kSteps; ++k) {
+                float o[V];
+                fma_vec<V>(h, f[k], h, add[k]);
+#pragma unroll
+                for (int v = 0; v < V; ++v) o[v] = k < n ? h[v] : 0.0f;
+                if (k < rows) store_vec<T, V>(k < n ? out + k * out_step : ph + (i0 + k) * p.h_t, o);
+            }
+        }
+    }
+    if (p.hT && at.own >= 0) p.hT[at.own] = carry;
+}
+
+template <typename T, int V, bool GATE>
+__global__ void __launch_bounds__(Shape<T, V, true>::kThreads, Shape<T, V, true>::kResident) linrec_wide_backward_kernel(const __grid_constant__ LinrecArgs p)
+{
+    typedef Shape<T, V, true> S;
+    constexpr int kSteps = S::kSteps, kWarps = S::kThreads / 32, kSpan = kWarps * kSteps, kC = 32 * V, kStates = kSpan / LSTM_LINREC_SEGMENT;
+    static_assert(kSpan % LSTM_LINREC_SEGMENT == 0 && LSTM_LINREC_SEGMENT % kSteps == 0, "a round begins at a saved state");
+    extern __shared__ __align__(16) unsigned char smem[];
+    __shared__ __align__(16) float mapA[kWarps][kC], mapH[kWarps][kC], mapQ[kWarps][kC], front[kWarps][kC], behind[kWarps][kC];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const Channels<V> at(p);
+    float carry = at.own >= 0 && p.h0 ? p.h0[at.own] : 0.0f;       // what reaches the state behind the steps that are left
+    const long long sign = p.reverse ? -1 : 1;
+    const long long step[3] = {sign * p.a_t, sign * p.x_t, sign * p.dh_t}, jump[3] = {kSpan * step[0], kSpan * step[1], kSpan * step[2]};
+    const long long rounds = ((long long)p.T + kSpan - 1) / kSpan;
+    long long base = (rounds - 1) * kSpan, i0 = base + warp * kSteps, ahead = i0;
+    const long long first = p.reverse ? at.len - 1 - i0 : i0;
+    const T *from[3] = {(const T *)p.a + at.b * p.a_b + at.d + first * p.a_t, (const T *)p.x + at.b * p.x_b + at.d + first * p.x_t,
+                        (const T *)p.dh + at.b * p.dh_b + at.d + first * p.dh_t};
+    T *pda = (T *)p.da + at.b * p.da_b + at.d, *pdx = (T *)p.h + at.b * p.h_b + at.d;
+    typedef Inputs<T, V, 3, GATE, true> In;
+    In in(smem);
+    auto fetch = [&]() {
+        in.fetch(from, step, count_steps<kSteps>(ahead, at.len));
+        ahead -= kSpan;
+#pragma unroll
+        for (int i = 0; i < 3; ++i) from[i] -= jump[i];
+    };
+#pragma unroll
+    for (int i = 0; i < In::kDepth; ++i) fetch();
+    float saved[kStates];
+    auto fetch_states = [&](long long of) {
+#pragma unroll
+        for (int s = 0; s < kStates; ++s) {
+            const long long i = of + s * LSTM_LINREC_SEGMENT;
+            saved[s] = at.own >= 0 && i >= 0 && i < p.T ? p.states[i / LSTM_LINREC_SEGMENT * at.BD + at.own] : 0.0f;
+        }
+    };
+    fetch_states(base);
+    for (; base >= 0; base -= kSpan, i0 -= kSpan) {
+        const int n = count_steps<kSteps>(i0, at.len);
+        in.next_if_registers();
+        fetch();
+        in.arrived();
+        float f[kSteps][V], w[kSteps][V];
+        float A[V], H[V], Q[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) { A[v] = 1.0f; H[v] = Q[v] = 0.0f; }
+#pragma unroll
+        for (int k = 0; k < kSteps; ++k) {
+            const Vec<T, V> ra = in.get_vec(0, k), rx = in.get_vec(1, k);
+            float x[V];
+#pragma unroll
+            for (int v = 0; v < V; ++v) { f[k][v] = get<T, V>(ra, v); x[v] = get<T, V>(rx, v); w[k][v] = 1.0f; }
+            if (GATE) {
+                gate_vec<T, V>(f[k], f[k], w[k]);
+                mul_vec<V>(x, x, w[k]);
+            }
+            fma_vec<V>(H, f[k], H, x);
+            mul_vec<V>(A, A, f[k]);
+        }
+#pragma unroll
+        for (int k = kSteps - 1; k >= 0; --k) {
+            const Vec<T, V> rd = in.get_vec(2, k);
+            float d[V];
+#pragma unroll
+            for (int v = 0; v < V; ++v) d[v] = get<T, V>(rd, v);
+            add_vec<V>(Q, Q, d);
+            mul_vec<V>(Q, Q, f[k]);
+        }
+#pragma unroll
+        for (int v = 0; v < V; ++v) A[v] = held<V, GATE>(A[v]);
+        store_vec<float, V>(&mapA[warp][lane * V], A);
+        store_vec<float, V>(&mapH[warp][lane * V], H);
+        store_vec<float, V>(&mapQ[warp][lane * V], Q);
+        __syncthreads();
+        if (threadIdx.x < kC) {
+            float a[kWarps], h[kWarps], q[kWarps], state = 0.0f;
+#pragma unroll
+            for (int i = 0; i < kWarps; ++i) { a[i] = mapA[i][threadIdx.x]; h[i] = mapH[i][threadIdx.x]; q[i] = mapQ[i][threadIdx.x]; }
+#pragma unroll
+            for (int i = 0; i < kWarps; ++i) {
+                if (i * kSteps % LSTM_LINREC_SEGMENT == 0) state = saved[i * kSteps / LSTM_LINREC_SEGMENT];
+                front[i][threadIdx.x] = state;
+                state = fmaf(a[i], state, h[i]);
+            }
+#pragma unroll
+            for (int i = kWarps - 1; i >= 0; --i) {
+                behind[i][threadIdx.x] = carry;
+                carry = fmaf(a[i], carry, q[i]);
+            }
+            fetch_states(base - kSpan);
+        }
+        __syncthreads();
+        const Vec<float, V> begin = load_vec<float, V>(&front[warp][lane * V]), end = load_vec<float, V>(&behind[warp][lane * V]);
+        float h[V], q[V], u[kSteps][V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) { h[v] = get<float, V>(begin, v); q[v] = get<float, V>(end, v); }
+        // da_t = g_t u_t and dx_t = g_t w_t with u = (h_{t-1} - x) f (1 - f), w = 1 - f  (decay: u = h_{t-1}, w = 1)
+#pragma unroll
+        for (int k = 0; k < kSteps; ++k) {
+            const Vec<T, V> rx = in.get_vec(1, k);
+            float x[V];
+#pragma unroll
+            for (int v = 0; v < V; ++v) { x[v] = get<T, V>(rx, v); u[k][v] = GATE ? h[v] - x[v] : h[v]; }
+            if (GATE) {
+                float fw[V];
+                mul_vec<V>(fw, f[k], w[k]);
+                mul_vec<V>(u[k], u[k], fw);
+                mul_vec<V>(x, x, w[k]);
+            }
+            fma_vec<V>(h, f[k], h, x);
+        }
+        const int rows = count_steps<kSteps>(i0, at.end);
+        const long long t0 = p.reverse ? at.len - 1 - i0 : i0;
+        T *qa = pda + t0 * p.da_t, *qx = pdx + t0 * p.h_t;
+#pragma unroll
+        for (int k = kSteps - 1; k >= 0; --k) {
+            const Vec<T, V> rd = in.get_vec(2, k);
+            float oa[V], ox[V], g[V];
+#pragma unroll
+            for (int v = 0; v < V; ++v) g[v] = get<T, V>(rd, v);
+            add_vec<V>(g, g, q);
+            mul_vec<V>(oa, g, u[k]);
+            mul_vec<V>(ox, g, w[k]);
+            mul_vec<V>(q, g, f[k]);
+            if (n == kSteps || k < n) {
+                store_vec<T, V>(qa + k * sign * p.da_t, oa);
+                store_vec<T, V>(qx + k * sign * p.h_t, ox);
+            } else if (k < rows) {
+                store_raw<T, V>(pda + (i0 + k) * p.da_t, zero_vec<T, V>());
+                store_raw<T, V>(pdx + (i0 + k) * p.h_t, zero_vec<T, V>());
+            }
+        }
+        in.next();
+    }
+    if (p.hT && at.own >= 0) p.hT[at.own] = carry;
+}
+
+template <typename T, int V, bool GATE>
+cudaError_t launch(LinrecArgs &p, bool backward, cudaStream_t st)
+{
+    p.nvec = p.D / V;
+    const void *fn = backward ? (const void *)linrec_wide_backward_kernel<T, V, GATE> : (const void *)linrec_wide_forward_kernel<T, V, GATE>;
+    const int smem = backward ? Inputs<T, V, 3, GATE, true>::kSmem : Inputs<T, V, 2, GATE, false>::kSmem;
+    static std::atomic<unsigned long long> prepared[2];
+    const cudaError_t e = prepare_kernel(fn, prepared[backward], smem, false);
+    if (e != cudaSuccess) return e;
+    const long long groups = ((long long)p.B * p.nvec + 31) / 32;
+    void *args[] = {&p};
+    return cudaLaunchKernel(fn, dim3((unsigned)groups), dim3(backward ? Shape<T, V, true>::kThreads : Shape<T, V, false>::kThreads), args, smem, st);
+}
+template <typename T>
+cudaError_t by_vector(LinrecArgs &p, int v, bool backward, cudaStream_t st)
+{
+    if (v == 4) return p.gate ? launch<T, 4, true>(p, backward, st) : launch<T, 4, false>(p, backward, st);
+    if (v == 2) return p.gate ? launch<T, 2, true>(p, backward, st) : launch<T, 2, false>(p, backward, st);
+    return p.gate ? launch<T, 1, true>(p, backward, st) : launch<T, 1, false>(p, backward, st);
+}
+
+}  // namespace
+
+bool linrec_wide_serves(const LinrecArgs &p, int v, bool bf16, bool backward, int sms, int &wide_v)
+{
+    const long long channels = (long long)p.B * p.D;
+    auto groups = [&](int n) { return (channels / n + 31) / 32; };
+    wide_v = v;
+    if (v == 4 && groups(4) < 2 * sms) wide_v = 2;
+    return groups(wide_v) * 5 >= 6ll * sms;
+}
+
+cudaError_t launch_linrec_wide(LinrecArgs &p, int v, bool bf16, bool backward, cudaStream_t st)
+{
+    return bf16 ? by_vector<__nv_bfloat16>(p, v, backward, st) : by_vector<float>(p, v, backward, st);
+}
+
+}  // namespace lstm

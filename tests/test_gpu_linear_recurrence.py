@@ -14,6 +14,9 @@ pytestmark = pytest.mark.gpu
 SHAPES = [(1, 1, 1), (1, 16, 1500), (2, 3, 7), (15, 2, 33), (16, 1, 2), (17, 2, 34), (63, 3, 5), (64, 1, 64), (65, 2, 130), (129, 1, 257),
           (257, 2, 32), (400, 16, 80), (700, 1, 100), (1023, 1, 31), (1025, 2, 48), (2049, 1, 50), (4097, 1, 66), (5000, 1, 37), (35, 20, 200),
           (33, 40, 1500), (3, 700, 66)]
+# many channels: vectors of four, two and one, rounds of 16, 32 and 64 steps that end anywhere
+SHAPES += [(1, 100, 600), (15, 80, 500), (16, 64, 640), (17, 50, 900), (47, 100, 400), (64, 40, 1000), (65, 30, 2000), (200, 60, 700),
+           (1, 80, 302), (31, 40, 602), (33, 100, 230), (129, 40, 602), (1, 30, 301), (16, 40, 151), (63, 20, 301), (65, 9, 701), (130, 20, 301)]
 MODES = list(itertools.product(("bf16", "fp32"), (True, False), (False, True), (False, True), ("plain", "fused", "batch_first")))
 
 
