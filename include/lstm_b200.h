@@ -404,13 +404,16 @@ enum { LSTM_BF16 = 2 };                      /* dtype of the operators' activati
  *   LSTM_LINREC_SEGMENT * k (behind a sequence's end, its last state); the backward pass reads it.
  * Decays above 1 are served as long as their product over the steps that count stays within the range of fp32.
  * T = 1 is the serving step: with hT = h0 the state is updated in place.
+ * workspace: lstm_linear_recurrence_workspace(T, B, D) floats (0 for most sizes: then NULL will do; -1: bad sizes) that
+ * nothing else uses until the call has run; the backward call needs as many.
  */
+LSTM_API long long lstm_linear_recurrence_workspace(int T, int B, int D);
 enum { LSTM_LINREC_GATE = 1, LSTM_LINREC_REVERSE = 2 };
 #define LSTM_LINREC_SEGMENT 16
 LSTM_API int lstm_linear_recurrence(const void *a, long long a_t, long long a_b, const void *x, long long x_t, long long x_b,
                                     const float *h0, const int *lengths, int T, int B, int D, int dtype, int flags,
                                     void *h, long long h_t, long long h_b, float *hT, float *states,
-                                    void *cuda_stream, char *err, int errlen);
+                                    float *workspace, long long workspace_floats, void *cuda_stream, char *err, int errlen);
 
 /*
  * Its gradients.  dh [T,B,D] is the gradient that reaches h, dhT [B,D] fp32 (or NULL: 0) the one that reaches hT:
@@ -424,7 +427,8 @@ LSTM_API int lstm_linear_recurrence_backward(const void *a, long long a_t, long 
                                              const float *states, const void *dh, long long dh_t, long long dh_b, const float *dhT,
                                              const int *lengths, int T, int B, int D, int dtype, int flags,
                                              void *da, long long da_t, long long da_b, void *dx, long long dx_t, long long dx_b,
-                                             float *dh0, void *cuda_stream, char *err, int errlen);
+                                             float *dh0, float *workspace, long long workspace_floats,
+                                             void *cuda_stream, char *err, int errlen);
 
 /*
  * Root-mean-square norm of rows, with the residual's addition in front:

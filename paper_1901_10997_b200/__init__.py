@@ -9,7 +9,7 @@ from .binding import (LSTM, HLSTM, LstmError, hlstm_create, lib_path, load_libra
                       lstm_forward, lstm_forward_host, lstm_input_projection, lstm_forward_noalloc, lstm_info, lstm_last_error,
                       lstm_probe, lstm_profile_enable, lstm_profile_read, lstm_selftest_timeout, lstm_status,
                       lstm_lhp_points, lstm_nearest_lhp, lstm_fold_input_affine, lstm_csr_lane_layout,
-                      lstm_linear_recurrence, lstm_linear_recurrence_backward, lstm_rms_norm, lstm_rms_norm_backward,
+                      lstm_linear_recurrence, lstm_linear_recurrence_backward, lstm_linear_recurrence_workspace, lstm_rms_norm, lstm_rms_norm_backward,
                       lstm_rms_norm_workspace, lstm_fp8_quantize, lstm_fp8_product,
                       LSTM_BF16, LSTM_LINREC_GATE, LSTM_LINREC_REVERSE, LSTM_LINREC_SEGMENT, LSTM_RMS_NORM_MAX_WIDTH,
                       LSTM_F32, LSTM_BF16W_F32S, LSTM_DENSE, LSTM_CSR, LSTM_OK, LSTM_ERR_INVALID,

@@ -100,10 +100,12 @@ def load_library():
         lib.lstm_csr_lane_layout.argtypes = [vp, vp, vp, ci, ci, ci, ci, ci, vp, vp, pi, ctypes.POINTER(ctypes.c_longlong)]
         ll, cf, text = ctypes.c_longlong, ctypes.c_float, [ctypes.c_char_p, ci]
         lib.lstm_linear_recurrence.restype = ci
-        lib.lstm_linear_recurrence.argtypes = [vp, ll, ll, vp, ll, ll, vp, vp, ci, ci, ci, ci, ci, vp, ll, ll, vp, vp, vp, *text]
+        lib.lstm_linear_recurrence.argtypes = [vp, ll, ll, vp, ll, ll, vp, vp, ci, ci, ci, ci, ci, vp, ll, ll, vp, vp, vp, ll, vp, *text]
+        lib.lstm_linear_recurrence_workspace.restype = ll
+        lib.lstm_linear_recurrence_workspace.argtypes = [ci, ci, ci]
         lib.lstm_linear_recurrence_backward.restype = ci
         lib.lstm_linear_recurrence_backward.argtypes = [vp, ll, ll, vp, ll, ll, vp, vp, ll, ll, vp, vp, ci, ci, ci, ci, ci, vp, ll, ll,
-                                                        vp, ll, ll, vp, vp, *text]
+                                                        vp, ll, ll, vp, vp, ll, vp, *text]
         lib.lstm_rms_norm.restype = ci
         lib.lstm_rms_norm.argtypes = [vp, ll, vp, ll, vp, cf, ci, ci, ci, vp, ll, vp, vp, ll, vp, *text]
         lib.lstm_rms_norm_workspace.restype = ll
@@ -265,16 +267,22 @@ def _with_reason(fn, *args):
     return rc, err.value.decode() if rc else ""
 
 
-def lstm_linear_recurrence(a, a_t, a_b, x, x_t, x_b, h0, lengths, T, B, D, dtype, flags, h, h_t, h_b, hT, states, stream=0):
+def lstm_linear_recurrence(a, a_t, a_b, x, x_t, x_b, h0, lengths, T, B, D, dtype, flags, h, h_t, h_b, hT, states, workspace=0,
+                           workspace_floats=0, stream=0):
     return _with_reason(load_library().lstm_linear_recurrence, a, a_t, a_b, x, x_t, x_b, h0, lengths,
-                        T, B, D, dtype, flags, h, h_t, h_b, hT, states, stream)
+                        T, B, D, dtype, flags, h, h_t, h_b, hT, states, workspace, workspace_floats, stream)
+
+
+def lstm_linear_recurrence_workspace(T, B, D):
+    """Floats of workspace that lstm_linear_recurrence and its backward call need (-1: bad sizes)."""
+    return load_library().lstm_linear_recurrence_workspace(T, B, D)
 
 
 def lstm_linear_recurrence_backward(a, a_t, a_b, x, x_t, x_b, states, dh, dh_t, dh_b, dhT, lengths, T, B, D, dtype, flags,
-                                    da, da_t, da_b, dx, dx_t, dx_b, dh0, stream=0):
+                                    da, da_t, da_b, dx, dx_t, dx_b, dh0, workspace=0, workspace_floats=0, stream=0):
     return _with_reason(load_library().lstm_linear_recurrence_backward, a, a_t, a_b, x, x_t, x_b, states,
                         dh, dh_t, dh_b, dhT, lengths, T, B, D, dtype, flags, da, da_t, da_b,
-                        dx, dx_t, dx_b, dh0, stream)
+                        dx, dx_t, dx_b, dh0, workspace, workspace_floats, stream)
 
 
 def lstm_rms_norm(x, x_ld, residual, residual_ld, w, eps, rows, width, dtype, y, y_ld, scales, r, r_ld, stream=0):

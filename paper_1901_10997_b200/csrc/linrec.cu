@@ -519,7 +519,7 @@ cudaError_t by_vector(LinrecArgs &p, bool backward, int sms, cudaStream_t st)
     matrix(p.hT, 0, 0, 4);
     matrix(p.states, 0, 0, 4);
     int wide_v;
-    if (linrec_wide_serves(p, v, sizeof(T) == 2, backward, sms, wide_v)) return launch_linrec_wide(p, wide_v, sizeof(T) == 2, backward, st);
+    if (linrec_wide_serves(p, v, sms, wide_v)) return launch_linrec_wide(p, wide_v, sizeof(T) == 2, backward, st);
     constexpr int kMost = 8 / sizeof(T);
     if (v >= kMost) return by_gate<T, kMost>(p, backward, sms, st);
     return v == 2 ? by_gate<T, 2>(p, backward, sms, st) : by_gate<T, 1>(p, backward, sms, st);
@@ -543,6 +543,15 @@ int check(const void *a, const void *x, int T, int B, int D, int dtype, int flag
     return LSTM_OK;
 }
 
+int take_workspace(LinrecArgs &p, float *workspace, long long floats, const Failure &fail)
+{
+    p.chunks = linrec_chunks(p.T, p.B, p.D, p.chunk_len);
+    p.maps = workspace;
+    if (p.chunks > 1 && (!workspace || !aligned_to(workspace, 4) || floats < 2ll * p.chunks * p.B * p.D))
+        return fail(LSTM_ERR_INVALID, "bad argument: the workspace is smaller than lstm_linear_recurrence_workspace says");
+    return LSTM_OK;
+}
+
 bool aligned(const void *p, int dtype) { return aligned_to(p, bytes_of(dtype)); }
 
 }  // namespace
@@ -552,9 +561,17 @@ using namespace lstm;
 
 extern "C" {
 
+long long lstm_linear_recurrence_workspace(int T, int B, int D)
+{
+    if (T < 0 || B < 0 || D < 1) return -1;
+    int chunk_len = 0;
+    const int chunks = linrec_chunks(T, B, D, chunk_len);
+    return chunks > 1 ? 2ll * chunks * B * D : 0;
+}
+
 int lstm_linear_recurrence(const void *a, long long a_t, long long a_b, const void *x, long long x_t, long long x_b, const float *h0,
                            const int *lengths, int T, int B, int D, int dtype, int flags, void *h, long long h_t, long long h_b, float *hT,
-                           float *states, void *cuda_stream, char *err, int errlen)
+                           float *states, float *workspace, long long workspace_floats, void *cuda_stream, char *err, int errlen)
 {
     const Failure fail{err, errlen};
     if (const int rc = check(a, x, T, B, D, dtype, flags, fail)) return rc;
@@ -572,13 +589,15 @@ int lstm_linear_recurrence(const void *a, long long a_t, long long a_b, const vo
     p.reverse = flags & LSTM_LINREC_REVERSE ? 1 : 0;
     p.h = h; p.h_t = h_t; p.h_b = h_b;
     p.hT = hT; p.states = states;
+    if (const int rc = take_workspace(p, workspace, workspace_floats, fail)) return rc;
     return run(p, dtype, false, (cudaStream_t)cuda_stream, fail);
 }
 
 int lstm_linear_recurrence_backward(const void *a, long long a_t, long long a_b, const void *x, long long x_t, long long x_b,
                                     const float *states, const void *dh, long long dh_t, long long dh_b, const float *dhT,
                                     const int *lengths, int T, int B, int D, int dtype, int flags, void *da, long long da_t, long long da_b,
-                                    void *dx, long long dx_t, long long dx_b, float *dh0, void *cuda_stream, char *err, int errlen)
+                                    void *dx, long long dx_t, long long dx_b, float *dh0, float *workspace, long long workspace_floats,
+                                    void *cuda_stream, char *err, int errlen)
 {
     const Failure fail{err, errlen};
     if (const int rc = check(a, x, T, B, D, dtype, flags, fail)) return rc;
@@ -598,6 +617,7 @@ int lstm_linear_recurrence_backward(const void *a, long long a_t, long long a_b,
     p.hT = dh0; p.states = const_cast<float *>(states);
     p.dh = dh; p.dh_t = dh_t; p.dh_b = dh_b;
     p.da = da; p.da_t = da_t; p.da_b = da_b;
+    if (const int rc = take_workspace(p, workspace, workspace_floats, fail)) return rc;
     return run(p, dtype, true, (cudaStream_t)cuda_stream, fail);
 }
 

@@ -11,6 +11,8 @@ struct LinrecArgs {
     const int *lengths;
     int T, B, D, nvec;          // vectors of channels per sequence
     int gate, reverse, csize;
+    int chunks, chunk_len;      // time cut into chunks that run side by side (linrec_wide.cu): T = chunks * chunk_len or less
+    float *maps;                // [2][chunks][B][D], where there is more than one
     void *h;                    // backward: dx
     long long h_t, h_b;
     float *hT;                  // [B][D]; backward: dh0
@@ -203,8 +205,10 @@ __device__ __forceinline__ int count_steps(long long i0, int last)
     return i0 < 0 || i0 >= last ? 0 : min(STEPS, last - (int)i0);
 }
 
-// The kernels for many channels (linrec_wide.cu); V channels are a vector.
-bool linrec_wide_serves(const LinrecArgs &p, int v, bool bf16, bool backward, int sms, int &wide_v);
+// The kernels for many channels, and for chunks of time (linrec_wide.cu); a vector has v channels.
+// How many chunks a call is cut into, and their length (a multiple of 64): the same for a call's workspace and its launch.
+int linrec_chunks(int T, int B, int D, int &chunk_len);
+bool linrec_wide_serves(const LinrecArgs &p, int v, int sms, int &wide_v);
 cudaError_t launch_linrec_wide(LinrecArgs &p, int v, bool bf16, bool backward, cudaStream_t st);
 
 }  // namespace lstm

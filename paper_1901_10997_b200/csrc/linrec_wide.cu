@@ -5,6 +5,10 @@
 // are resident to keep the memory busy, which is what bounds it: 2048 x 32 x 1500 of bf16 takes 109 us, 0.82 of the copy rate
 // (the kernels of linrec.cu, which can spread one sequence over a cluster, 165).
 //
+// Few channels and many steps: time is cut into chunks that run side by side like further sequences.  A first kernel reduces every
+// chunk to its map (reading the inputs once more than they would have to be, and nothing of what the second one writes), and in front
+// of its first round a CTA of the second runs through the maps of the chunks before its own.
+//
 // Backward: a round's spans begin at saved states, so the same pass over the maps gives the states in front of the spans (from the
 // saved ones, forwards) and the gradients that arrive behind them (from the carry, backwards).
 #include "../../include/lstm_b200.h"
@@ -29,26 +33,133 @@ template <typename T> struct Shape<T, 1, true> { static constexpr int kSteps = 8
 template <typename T, int V, int N, bool GATE, bool BACK, typename S = Shape<T, V, BACK>>
 using Inputs = std::conditional_t<S::kDepth == 0, InRegisters<T, V, N, GATE, S::kSteps>, InShared<T, V, N, GATE, S::kSteps, S::kThreads, S::kDepth ? S::kDepth : 1>>;
 
-// a lane's channels, and the one channel whose carry a thread keeps
+// a lane's channels of one chunk of time, and the one channel whose carry a thread keeps
 template <int V>
 struct Channels {
-    int b, d, len, end;         // steps of the sequence; of the batch (0 where there is no such channel)
-    long long bd, BD, own;      // own: [B][D] index of channel threadIdx.x of the CTA, or -1
+    int b, d, len;              // len: steps of the sequence
+    int off, stop, end;         // the chunk's first step, its last of the sequence and of the batch (0 where there is no such channel)
+    long long bd, BD;
     bool live;
+    long long own, own_map;     // channel threadIdx.x of the CTA: index into [B][D] (-1: none) and into [chunks][B][D]
+    int own_chunk;
     __device__ explicit Channels(const LinrecArgs &p)
     {
-        const long long all = (long long)p.B * p.nvec, vec = (long long)blockIdx.x * 32 + (threadIdx.x & 31);
+        const long long all = (long long)p.chunks * p.B * p.nvec, vec = (long long)blockIdx.x * 32 + (threadIdx.x & 31);
         live = vec < all;
-        b = live ? (int)(vec / p.nvec) : 0;
+        const long long cb = live ? vec / p.nvec : 0;
+        const int chunk = (int)(cb / p.B);
+        b = (int)(cb % p.B);
         d = live ? (int)(vec % p.nvec) * V : 0;
         len = !live ? 0 : p.lengths ? min(max(p.lengths[b], 0), p.T) : p.T;
-        end = live ? p.T : 0;
+        off = chunk * p.chunk_len;
+        end = live ? (int)min((long long)p.T, (long long)off + p.chunk_len) : 0;
+        stop = min(len, end);
         bd = (long long)b * p.D + d;
         BD = (long long)p.B * p.D;
         const long long mine = (long long)blockIdx.x * 32 + threadIdx.x / V;
-        own = threadIdx.x < 32 * V && mine < all ? mine / p.nvec * p.D + mine % p.nvec * V + threadIdx.x % V : -1;
+        own = own_map = -1;
+        own_chunk = 0;
+        if (threadIdx.x < 32 * V && mine < all) {
+            const long long mcb = mine / p.nvec;
+            const int md = (int)(mine % p.nvec) * V + threadIdx.x % V;
+            own_chunk = (int)(mcb / p.B);
+            own = mcb % p.B * p.D + md;
+            own_map = mcb * p.D + md;
+        }
     }
 };
+
+// The carry of a thread's channel in front of its chunk: the initial one behind the maps of the chunks on the way.
+__device__ __forceinline__ float carry_before(const LinrecArgs &p, long long own, int chunk, bool backward)
+{
+    if (own < 0) return 0.0f;
+    float carry = p.h0 ? p.h0[own] : 0.0f;
+    const long long BD = (long long)p.B * p.D, plane = p.chunks * BD;
+    const int way = backward ? p.chunks - 1 - chunk : chunk;
+#pragma unroll 8
+    for (int i = 0; i < way; ++i) {
+        const float *m = p.maps + (backward ? p.chunks - 1 - i : i) * BD + own;
+        carry = fmaf(m[0], carry, m[plane]);
+    }
+    return carry;
+}
+
+// The map of each chunk: of h (forward, from a and x), of what reaches the state in front of it (backward, from a and dh).  A warp has a
+// quarter of the chunk and four channels a lane, or as many as a vector has; the four meet once, at the end.
+template <typename T, int V, bool GATE, bool BACK>
+__global__ void __launch_bounds__(128, 5) linrec_chunk_maps_kernel(const __grid_constant__ LinrecArgs p)
+{
+    constexpr int kSteps = 4, kC = 32 * V;
+    typedef std::conditional_t<sizeof(T) * V == 2, InRegisters<T, V, 2, GATE, kSteps>, InShared<T, V, 2, GATE, kSteps, 128, 2>> In;
+    extern __shared__ __align__(16) unsigned char smem[];
+    __shared__ __align__(16) float mapA[4][kC], mapH[4][kC];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const Channels<V> at(p);
+    const long long sign = p.reverse ? -1 : 1, way = BACK ? -kSteps : kSteps;
+    const long long sa = sign * p.a_t, sx = sign * (BACK ? p.dh_t : p.x_t);
+    const long long step[2] = {sa, sx};
+    const int quarter = p.chunk_len / 4;
+    long long ahead = at.off + warp * quarter + (BACK ? quarter - kSteps : 0);
+    const long long first = p.reverse ? at.len - 1 - ahead : ahead;
+    const T *from[2] = {(const T *)p.a + at.b * p.a_b + at.d + first * p.a_t,
+                        BACK ? (const T *)p.dh + at.b * p.dh_b + at.d + first * p.dh_t : (const T *)p.x + at.b * p.x_b + at.d + first * p.x_t};
+    In in(smem);
+    int left = quarter;                 // steps of the quarter that are still to be fetched
+    auto fetch = [&]() {
+        in.fetch(from, step, left > 0 ? count_steps<kSteps>(ahead, at.stop) : 0);
+        left -= kSteps;
+        ahead += way;
+        from[0] += way * sa;
+        from[1] += way * sx;
+    };
+#pragma unroll
+    for (int i = 0; i < In::kDepth; ++i) fetch();
+    float A[V], H[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) { A[v] = 1.0f; H[v] = 0.0f; }
+    for (int i = 0; i < quarter; i += kSteps) {
+        in.next_if_registers();
+        fetch();
+        in.arrived();
+#pragma unroll
+        for (int kk = 0; kk < kSteps; ++kk) {
+            const int k = BACK ? kSteps - 1 - kk : kk;
+            const Vec<T, V> ra = in.get_vec(0, k), rx = in.get_vec(1, k);
+            float f[V], x[V];
+#pragma unroll
+            for (int v = 0; v < V; ++v) { f[v] = get<T, V>(ra, v); x[v] = get<T, V>(rx, v); }
+            if (GATE) {
+                float w[V];
+                gate_vec<T, V>(f, f, w);
+                if (!BACK) mul_vec<V>(x, x, w);
+            }
+            if (BACK) {
+                add_vec<V>(H, H, x);
+                mul_vec<V>(H, H, f);
+            } else {
+                fma_vec<V>(H, f, H, x);
+            }
+            mul_vec<V>(A, A, f);
+        }
+        in.next();
+#pragma unroll
+        for (int v = 0; v < V; ++v) A[v] = held<V, GATE>(A[v]);
+    }
+    store_vec<float, V>(&mapA[warp][lane * V], A);
+    store_vec<float, V>(&mapH[warp][lane * V], H);
+    __syncthreads();
+    if (at.own_map >= 0) {
+        float a = 1.0f, h = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int w = BACK ? 3 - i : i;
+            h = fmaf(mapA[w][threadIdx.x], h, mapH[w][threadIdx.x]);
+            a = held<V, GATE>(a * mapA[w][threadIdx.x]);
+        }
+        p.maps[at.own_map] = a;
+        p.maps[(long long)p.chunks * at.BD + at.own_map] = h;
+    }
+}
 
 template <typename T, int V, bool GATE>
 __global__ void __launch_bounds__(Shape<T, V, false>::kThreads, Shape<T, V, false>::kResident) linrec_wide_forward_kernel(const __grid_constant__ LinrecArgs p)
@@ -59,25 +170,25 @@ __global__ void __launch_bounds__(Shape<T, V, false>::kThreads, Shape<T, V, fals
     __shared__ __align__(16) float mapA[kWarps][kC], mapH[kWarps][kC], front[kWarps][kC];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const Channels<V> at(p);
-    float carry = at.own >= 0 && p.h0 ? p.h0[at.own] : 0.0f;
     const long long sign = p.reverse ? -1 : 1;
     const long long step[2] = {sign * p.a_t, sign * p.x_t}, jump[2] = {kSpan * step[0], kSpan * step[1]}, out_step = sign * p.h_t, out_jump = kSpan * out_step;
-    long long i0 = warp * kSteps, ahead = i0;
+    long long i0 = at.off + warp * kSteps, ahead = i0;
     const long long first = p.reverse ? at.len - 1 - i0 : i0;
     const T *from[2] = {(const T *)p.a + at.b * p.a_b + at.d + first * p.a_t, (const T *)p.x + at.b * p.x_b + at.d + first * p.x_t};
     T *ph = (T *)p.h + at.b * p.h_b + at.d, *out = ph + first * p.h_t;
     typedef Inputs<T, V, 2, GATE, false> In;
     In in(smem);
     auto fetch = [&]() {
-        in.fetch(from, step, count_steps<kSteps>(ahead, at.len));
+        in.fetch(from, step, count_steps<kSteps>(ahead, at.stop));
         ahead += kSpan;
         from[0] += jump[0];
         from[1] += jump[1];
     };
 #pragma unroll
     for (int i = 0; i < In::kDepth; ++i) fetch();
-    for (long long base = 0; base < p.T; base += kSpan, i0 += kSpan, out += out_jump) {
-        const int n = count_steps<kSteps>(i0, at.len);
+    float carry = carry_before(p, at.own, at.own_chunk, false);
+    for (long long base = 0; base < p.chunk_len; base += kSpan, i0 += kSpan, out += out_jump) {
+        const int n = count_steps<kSteps>(i0, at.stop);
         in.next_if_registers();
         fetch();
         in.arrived();
@@ -145,7 +256,7 @@ __global__ void __launch_bounds__(Shape<T, V, false>::kThreads, Shape<T, V, fals
             }
         }
     }
-    if (p.hT && at.own >= 0) p.hT[at.own] = carry;
+    if (p.hT && at.own >= 0 && at.own_chunk == p.chunks - 1) p.hT[at.own] = carry;
 }
 
 template <typename T, int V, bool GATE>
@@ -158,11 +269,10 @@ __global__ void __launch_bounds__(Shape<T, V, true>::kThreads, Shape<T, V, true>
     __shared__ __align__(16) float mapA[kWarps][kC], mapH[kWarps][kC], mapQ[kWarps][kC], front[kWarps][kC], behind[kWarps][kC];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const Channels<V> at(p);
-    float carry = at.own >= 0 && p.h0 ? p.h0[at.own] : 0.0f;       // what reaches the state behind the steps that are left
     const long long sign = p.reverse ? -1 : 1;
     const long long step[3] = {sign * p.a_t, sign * p.x_t, sign * p.dh_t}, jump[3] = {kSpan * step[0], kSpan * step[1], kSpan * step[2]};
-    const long long rounds = ((long long)p.T + kSpan - 1) / kSpan;
-    long long base = (rounds - 1) * kSpan, i0 = base + warp * kSteps, ahead = i0;
+    const long long rounds = ((long long)p.chunk_len + kSpan - 1) / kSpan;
+    long long base = (rounds - 1) * kSpan, i0 = at.off + base + warp * kSteps, ahead = i0;
     const long long first = p.reverse ? at.len - 1 - i0 : i0;
     const T *from[3] = {(const T *)p.a + at.b * p.a_b + at.d + first * p.a_t, (const T *)p.x + at.b * p.x_b + at.d + first * p.x_t,
                         (const T *)p.dh + at.b * p.dh_b + at.d + first * p.dh_t};
@@ -170,7 +280,7 @@ __global__ void __launch_bounds__(Shape<T, V, true>::kThreads, Shape<T, V, true>
     typedef Inputs<T, V, 3, GATE, true> In;
     In in(smem);
     auto fetch = [&]() {
-        in.fetch(from, step, count_steps<kSteps>(ahead, at.len));
+        in.fetch(from, step, count_steps<kSteps>(ahead, at.stop));
         ahead -= kSpan;
 #pragma unroll
         for (int i = 0; i < 3; ++i) from[i] -= jump[i];
@@ -181,13 +291,14 @@ __global__ void __launch_bounds__(Shape<T, V, true>::kThreads, Shape<T, V, true>
     auto fetch_states = [&](long long of) {
 #pragma unroll
         for (int s = 0; s < kStates; ++s) {
-            const long long i = of + s * LSTM_LINREC_SEGMENT;
+            const long long i = (long long)at.own_chunk * p.chunk_len + of + s * LSTM_LINREC_SEGMENT;
             saved[s] = at.own >= 0 && i >= 0 && i < p.T ? p.states[i / LSTM_LINREC_SEGMENT * at.BD + at.own] : 0.0f;
         }
     };
     fetch_states(base);
+    float carry = carry_before(p, at.own, at.own_chunk, true);      // what reaches the state behind the steps that are left
     for (; base >= 0; base -= kSpan, i0 -= kSpan) {
-        const int n = count_steps<kSteps>(i0, at.len);
+        const int n = count_steps<kSteps>(i0, at.stop);
         in.next_if_registers();
         fetch();
         in.arrived();
@@ -283,7 +394,7 @@ __global__ void __launch_bounds__(Shape<T, V, true>::kThreads, Shape<T, V, true>
         }
         in.next();
     }
-    if (p.hT && at.own >= 0) p.hT[at.own] = carry;
+    if (p.hT && at.own >= 0 && at.own_chunk == 0) p.hT[at.own] = carry;
 }
 
 template <typename T, int V, bool GATE>
@@ -295,8 +406,17 @@ cudaError_t launch(LinrecArgs &p, bool backward, cudaStream_t st)
     static std::atomic<unsigned long long> prepared[2];
     const cudaError_t e = prepare_kernel(fn, prepared[backward], smem, false);
     if (e != cudaSuccess) return e;
-    const long long groups = ((long long)p.B * p.nvec + 31) / 32;
+    const long long groups = ((long long)p.chunks * p.B * p.nvec + 31) / 32;
+    if (groups > 0x7fffffffll) return cudaErrorInvalidConfiguration;
     void *args[] = {&p};
+    if (p.chunks > 1) {
+        const void *maps = backward ? (const void *)linrec_chunk_maps_kernel<T, V, GATE, true> : (const void *)linrec_chunk_maps_kernel<T, V, GATE, false>;
+        constexpr int kMapSmem = sizeof(T) * V == 2 ? 0 : InShared<T, V, 2, GATE, 4, 128, 2>::kSmem;
+        static std::atomic<unsigned long long> maps_prepared[2];
+        cudaError_t e2 = prepare_kernel(maps, maps_prepared[backward], kMapSmem, false);
+        if (e2 == cudaSuccess) e2 = cudaLaunchKernel(maps, dim3((unsigned)groups), dim3(128), args, kMapSmem, st);
+        if (e2 != cudaSuccess) return e2;
+    }
     return cudaLaunchKernel(fn, dim3((unsigned)groups), dim3(backward ? Shape<T, V, true>::kThreads : Shape<T, V, false>::kThreads), args, smem, st);
 }
 template <typename T>
@@ -309,13 +429,29 @@ cudaError_t by_vector(LinrecArgs &p, int v, bool backward, cudaStream_t st)
 
 }  // namespace
 
-bool linrec_wide_serves(const LinrecArgs &p, int v, bool bf16, bool backward, int sms, int &wide_v)
+// Chunks pay where channels alone do not fill the chip and the work is large enough for a second launch and a second reading, most of
+// which comes from L2 up to some ten million elements.  us, cluster of CTAs (linrec.cu) / chunks: 65536 x 1 x 1500 of bf16 261 / 200,
+// backward 529 / 320; 16384 x 1 x 1500 69 / 59; 4096 x 4 x 1000 52 / 41; 65536 x 1 x 256 102 / 48; 4096 x 1 x 1500 20 / 21.
+// As many chunks as make some 48000 channels side by side, and no more than 64: each has to run through the maps of those before it.
+int linrec_chunks(int T, int B, int D, int &chunk_len)
 {
-    const long long channels = (long long)p.B * p.D;
+    chunk_len = T;
+    const long long channels = (long long)B * D;
+    if (channels > 11000 || channels * T < 8000000 || T < 512) return 1;
+    const int want = (int)(48000 / channels < 2 ? 2 : 48000 / channels > 64 ? 64 : 48000 / channels);
+    const long long len = (((long long)T + want - 1) / want + 63) / 64 * 64;
+    chunk_len = (int)len;
+    return (int)((T + len - 1) / len);
+}
+
+// Without chunks: where vectors of four make two CTAs an SM, else with vectors of two where those make more than one.
+bool linrec_wide_serves(const LinrecArgs &p, int v, int sms, int &wide_v)
+{
+    const long long channels = (long long)p.chunks * p.B * p.D;
     auto groups = [&](int n) { return (channels / n + 31) / 32; };
     wide_v = v;
     if (v == 4 && groups(4) < 2 * sms) wide_v = 2;
-    return groups(wide_v) * 5 >= 6ll * sms;
+    return p.chunks > 1 || groups(wide_v) * 5 >= 6ll * sms;
 }
 
 cudaError_t launch_linrec_wide(LinrecArgs &p, int v, bool bf16, bool backward, cudaStream_t st)

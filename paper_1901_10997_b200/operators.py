@@ -96,6 +96,12 @@ def _apart(t, name):
 
 
 # ---------------------------------------------------------------- recurrence
+def _workspace(T, B, D, like):
+    """A call's workspace, or None.  It is held until the call has been enqueued; torch's allocator orders its next use behind that."""
+    need = _b.lstm_linear_recurrence_workspace(T, B, D) if T > 64 else 0
+    return torch.empty((need,), dtype=_F32, device=like.device) if need > 0 else None
+
+
 def linear_recurrence(a, x, h0=None, lengths=None, *, gate=True, reverse=False, save=False, out=None, state=None):
     """h_t = f_t h_{t-1} + (1 - f_t) x_t with f = sigmoid(a), or (``gate`` false) h_t = a_t h_{t-1} + x_t.
 
@@ -114,6 +120,7 @@ def linear_recurrence(a, x, h0=None, lengths=None, *, gate=True, reverse=False, 
     if state is None:
         state = torch.empty(rows, dtype=_F32, device=a.device)
     states = torch.empty((-(-T // LSTM_LINREC_SEGMENT), B, D), dtype=_F32, device=a.device) if save else None
+    work = _workspace(T, B, D, a)
     a_t, a_b, _ = a.stride()
     px = _ptr(x, "x", shape, dtype, dev)
     x_t, x_b, _ = x.stride()
@@ -121,7 +128,8 @@ def linear_recurrence(a, x, h0=None, lengths=None, *, gate=True, reverse=False, 
     o_t, o_b, _ = out.stride()
     _call("lstm_linear_recurrence", dev, _ptr(a, "a", shape, dtype, dev), a_t, a_b, px, x_t, x_b, _whole(h0, "h0", rows, _F32, dev),
           _whole(lengths, "lengths", (B,), _I32, dev), T, B, D, dt, (LSTM_LINREC_GATE if gate else 0) | (LSTM_LINREC_REVERSE if reverse else 0),
-          po, o_t, o_b, _whole(state, "state", rows, _F32, dev), 0 if states is None else states.data_ptr())
+          po, o_t, o_b, _whole(state, "state", rows, _F32, dev), 0 if states is None else states.data_ptr(), 0 if work is None else work.data_ptr(),
+          0 if work is None else work.numel())
     return out, state, states
 
 
@@ -134,13 +142,15 @@ def linear_recurrence_backward(a, x, states, dh, dhT=None, lengths=None, *, gate
     rows = (B, D)
     da, dx = torch.empty(shape, dtype=dtype, device=a.device), torch.empty(shape, dtype=dtype, device=a.device)
     dh0 = torch.empty(rows, dtype=_F32, device=a.device)
+    work = _workspace(T, B, D, a)
     px, pd = _ptr(x, "x", shape, dtype, dev), _ptr(dh, "dh", shape, dtype, dev)
     if states is None:
         raise ValueError("states must be those that linear_recurrence saved")
     _call("lstm_linear_recurrence_backward", dev, _ptr(a, "a", shape, dtype, dev), a.stride(0), a.stride(1), px, x.stride(0), x.stride(1),
           _whole(states, "states", (-(-T // LSTM_LINREC_SEGMENT), B, D), _F32, dev), pd, dh.stride(0), dh.stride(1), _whole(dhT, "dhT", rows, _F32, dev),
           _whole(lengths, "lengths", (B,), _I32, dev), T, B, D, dt, (LSTM_LINREC_GATE if gate else 0) | (LSTM_LINREC_REVERSE if reverse else 0),
-          da.data_ptr(), B * D, D, dx.data_ptr(), B * D, D, dh0.data_ptr())
+          da.data_ptr(), B * D, D, dx.data_ptr(), B * D, D, dh0.data_ptr(), 0 if work is None else work.data_ptr(),
+          0 if work is None else work.numel())
     return da, dx, dh0
 
 

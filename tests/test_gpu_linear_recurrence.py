@@ -17,6 +17,8 @@ SHAPES = [(1, 1, 1), (1, 16, 1500), (2, 3, 7), (15, 2, 33), (16, 1, 2), (17, 2, 
 # many channels: vectors of four, two and one, rounds of 16, 32 and 64 steps that end anywhere
 SHAPES += [(1, 100, 600), (15, 80, 500), (16, 64, 640), (17, 50, 900), (47, 100, 400), (64, 40, 1000), (65, 30, 2000), (200, 60, 700),
            (1, 80, 302), (31, 40, 602), (33, 100, 230), (129, 40, 602), (1, 30, 301), (16, 40, 151), (63, 20, 301), (65, 9, 701), (130, 20, 301)]
+# few channels and many steps: chunks of time side by side
+CHUNKED = [(8200, 1, 1000), (4100, 2, 1002), (2100, 5, 801)]
 MODES = list(itertools.product(("bf16", "fp32"), (True, False), (False, True), (False, True), ("plain", "fused", "batch_first")))
 
 
@@ -24,6 +26,10 @@ def cases():
     r = random.Random(11)
     for shape in SHAPES:
         for mode in r.sample(MODES, 5):
+            yield (*shape, *mode)
+    for shape in CHUNKED:
+        assert pkg.lstm_linear_recurrence_workspace(*shape) > 0
+        for mode in (("bf16", True, True, True, "fused"), ("fp32", False, False, True, "plain"), ("bf16", True, False, False, "batch_first")):
             yield (*shape, *mode)
 
 
@@ -247,9 +253,10 @@ def test_offsets_beyond_32_bits():
         assert torch.equal(p, q)
 
 
-def test_recorded_and_on_two_streams():
+@pytest.mark.parametrize("shape", ((900, 2, 64), (40, 40, 600), (4100, 2, 1000)), ids=str)
+def test_recorded_and_on_two_streams(shape):
     """Calls keep nothing: recorded twice, replayed beside ordinary calls on another stream, all give the same bits."""
-    sets = [make(900, 2, 64, "bf16", True, True, "fused", s) for s in (11, 12)]
+    sets = [make(*shape, "bf16", True, True, "fused", s) for s in (11, 12)]
 
     def both(s):
         a, x, h0, lengths, dh, dhT = s
@@ -278,6 +285,18 @@ def test_recorded_and_on_two_streams():
         torch.cuda.synchronize()
         for got, w in ((outs[0], want[0]), (outs[1], want[1]), (other, want[0]), (here, want[1])):
             assert all(torch.equal(p, q) for p, q in zip(got, w))
+
+
+def test_a_workspace_that_is_too_small_is_refused():
+    T, B, D = CHUNKED[0]
+    need = pkg.lstm_linear_recurrence_workspace(T, B, D)
+    assert pkg.lstm_linear_recurrence_workspace(1, 4, 100) == 0 and pkg.lstm_linear_recurrence_workspace(-1, 4, 100) == -1
+    t = torch.zeros(T, B, D, device="cuda")
+    work, h = torch.empty(need, device="cuda"), torch.empty_like(t)
+    call = lambda at, n: pkg.lstm_linear_recurrence(t.data_ptr(), D, D, t.data_ptr(), D, D, 0, 0, T, B, D, pkg.LSTM_F32, 1, h.data_ptr(), D, D, 0, 0, at, n,
+                                                    torch.cuda.current_stream().cuda_stream)
+    assert call(0, need)[0] == pkg.LSTM_ERR_INVALID and call(work.data_ptr(), need - 1)[0] == pkg.LSTM_ERR_INVALID
+    assert call(work.data_ptr(), need) == (pkg.LSTM_OK, "")
 
 
 def test_tensors_that_do_not_fit_are_refused():
