@@ -397,10 +397,55 @@ __global__ void __launch_bounds__(Shape<T, V, true>::kThreads, Shape<T, V, true>
     if (p.hT && at.own >= 0 && at.own_chunk == 0) p.hT[at.own] = carry;
 }
 
+// Up to four steps (generation): a thread runs through its vector's steps alone, nothing is joined.
+constexpr int kShort = 4;
+template <typename T, int V, bool GATE>
+__global__ void __launch_bounds__(64) linrec_short_kernel(const __grid_constant__ LinrecArgs p)
+{
+    const long long vec = (long long)blockIdx.x * 64 + threadIdx.x;
+    if (vec >= (long long)p.B * p.nvec) return;
+    const int b = (int)(vec / p.nvec), d = (int)(vec % p.nvec) * V;
+    const int len = p.lengths ? min(max(p.lengths[b], 0), p.T) : p.T;
+    const long long bd = (long long)b * p.D + d, sign = p.reverse ? -1 : 1, first = p.reverse ? len - 1 : 0;
+    const T *pa = (const T *)p.a + b * p.a_b + d + first * p.a_t, *px = (const T *)p.x + b * p.x_b + d + first * p.x_t;
+    T *ph = (T *)p.h + b * p.h_b + d;
+    Vec<T, V> ra[kShort], rx[kShort];
+    float h[V];
+#pragma unroll
+    for (int k = 0; k < kShort; ++k) {
+        if (k >= p.T) break;
+        ra[k] = k < len ? load_vec<T, V>(pa + k * sign * p.a_t) : keep<T, V, GATE>();
+        rx[k] = k < len ? load_vec<T, V>(px + k * sign * p.x_t) : zero_vec<T, V>();
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) h[v] = p.h0 ? p.h0[bd + v] : 0.0f;
+    if (p.states) store_vec<float, V>(p.states + bd, h);
+#pragma unroll
+    for (int k = 0; k < kShort; ++k) {
+        if (k >= p.T) break;
+        float f[V], x[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) { f[v] = get<T, V>(ra[k], v); x[v] = get<T, V>(rx[k], v); }
+        if (GATE) {
+            float w[V];
+            gate_vec<T, V>(f, f, w);
+            mul_vec<V>(x, x, w);
+        }
+        fma_vec<V>(h, f, h, x);
+        if (k < len) store_vec<T, V>(ph + (first + k * sign) * p.h_t, h);
+        else store_raw<T, V>(ph + k * p.h_t, zero_vec<T, V>());
+    }
+    if (p.hT) store_vec<float, V>(p.hT + bd, h);
+}
+
 template <typename T, int V, bool GATE>
 cudaError_t launch(LinrecArgs &p, bool backward, cudaStream_t st)
 {
     p.nvec = p.D / V;
+    if (!backward && p.T <= kShort) {
+        linrec_short_kernel<T, V, GATE><<<(unsigned)(((long long)p.B * p.nvec + 63) / 64), 64, 0, st>>>(p);
+        return cudaGetLastError();
+    }
     const void *fn = backward ? (const void *)linrec_wide_backward_kernel<T, V, GATE> : (const void *)linrec_wide_forward_kernel<T, V, GATE>;
     const int smem = backward ? Inputs<T, V, 3, GATE, true>::kSmem : Inputs<T, V, 2, GATE, false>::kSmem;
     static std::atomic<unsigned long long> prepared[2];
@@ -445,11 +490,12 @@ int linrec_chunks(int T, int B, int D, int &chunk_len)
 }
 
 // Without chunks: where vectors of four make two CTAs an SM, else with vectors of two where those make more than one.
-bool linrec_wide_serves(const LinrecArgs &p, int v, int sms, int &wide_v)
+bool linrec_wide_serves(const LinrecArgs &p, int v, bool backward, int sms, int &wide_v)
 {
     const long long channels = (long long)p.chunks * p.B * p.D;
     auto groups = [&](int n) { return (channels / n + 31) / 32; };
     wide_v = v;
+    if (p.T <= kShort && !backward) return true;
     if (v == 4 && groups(4) < 2 * sms) wide_v = 2;
     return p.chunks > 1 || groups(wide_v) * 5 >= 6ll * sms;
 }
