@@ -80,6 +80,7 @@ __device__ __forceinline__ void cluster_sync()
 constexpr int kFewThreads = 192;
 constexpr int kFewSmem = 108 * 1024;
 constexpr int kMaxStages = 12;
+constexpr int kMaxSplit = 8;          // CTAs that share a tile
 
 template <typename T, int R>
 __global__ void __launch_bounds__(kFewThreads)
@@ -189,24 +190,30 @@ fp8_few_rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
     const int n = n_tile * kTileOuts + tid;
     T *y = (T *)p.y;
     if (p.csize > 1) {
-        // all blocks have been multiplied: the stages' memory takes this CTA's sums
-        float *part = reinterpret_cast<float *>(smem_raw + (tiles - smem_u32(smem_raw)));
+        // all blocks have been multiplied: the stages' memory takes this CTA's sums, four rows of x side by side for each row of w
+        float4 *part = reinterpret_cast<float4 *>(smem_raw + (tiles - smem_u32(smem_raw)));
         if (warp < 4) {
 #pragma unroll
-            for (int r = 0; r < R; ++r) part[r * kTileOuts + tid] = sum[r];
+            for (int r = 0; r < R; r += 4) part[r / 4 * kTileOuts + tid] = make_float4(sum[r], sum[r + 1], sum[r + 2], sum[r + 3]);
         }
         cluster_sync();
         if (warp < 4 && n < p.outs) {
             const float b = p.bias ? p.bias[n] : 0.0f;
-            const uint32_t here = tiles + (uint32_t)tid * 4;
-            for (int r = rank; r < R && m0 + r < p.rows; r += p.csize) {
-                float v = 0.0f;
-                for (int c = 0; c < p.csize; ++c) {
-                    float u;
-                    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(u) : "r"(at_rank(here + r * kTileOuts * 4, c)) : "memory");
-                    v += u;
-                }
-                y[(long long)(m0 + r) * p.y_ld + n] = T(v + b);
+            const uint32_t here = tiles + (uint32_t)tid * 16;
+            for (int q = rank; q < R / 4 && m0 + 4 * q < p.rows; q += p.csize) {
+                float4 u[kMaxSplit];                     // all on their way before the first is added
+#pragma unroll
+                for (int c = 0; c < kMaxSplit; ++c)
+                    if (c < p.csize)
+                        asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                                     : "=f"(u[c].x), "=f"(u[c].y), "=f"(u[c].z), "=f"(u[c].w) : "r"(at_rank(here + q * kTileOuts * 16, c)) : "memory");
+                float v[4] = {u[0].x, u[0].y, u[0].z, u[0].w};
+#pragma unroll
+                for (int c = 1; c < kMaxSplit; ++c)
+                    if (c < p.csize) { v[0] += u[c].x; v[1] += u[c].y; v[2] += u[c].z; v[3] += u[c].w; }
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (m0 + 4 * q + k < p.rows) y[(long long)(m0 + 4 * q + k) * p.y_ld + n] = T(v[k] + b);
             }
         }
         cluster_sync();                                  // nobody's memory goes while another reads it
@@ -230,7 +237,10 @@ cudaError_t launch_few(ProductArgs &p, const CUtensorMap &mw, const CUtensorMap 
     const void *fn = (const void *)fp8_few_rows_kernel<T, R>;
     const int n_tiles = (p.outs + kTileOuts - 1) / kTileOuts, m_tiles = (p.rows + R - 1) / R;
     const long long tiles = (long long)n_tiles * m_tiles;
-    p.csize = (int)(sms / tiles < 1 ? 1 : sms / tiles > 8 ? 8 : sms / tiles);
+    // CTAs for one and a half of the SMs: with fewer some SMs read nothing, with more the joining costs more than their reading saves
+    // (64 x 6000 x 1500: 3 CTAs a tile 13.4 us, 4 10.6, 6 20.2)
+    const long long share = 3ll * sms / (2 * tiles);
+    p.csize = (int)(share < 1 ? 1 : share > kMaxSplit ? kMaxSplit : share);
     if (p.csize > p.blocks) p.csize = p.blocks;
     constexpr int kStage = kTileOuts * kBlockK + R * kBlockK;
     // two CTAs of an SM share its memory; the sums of a split tile need the first R / 32 stages' worth
@@ -553,10 +563,13 @@ template <typename T>
 cudaError_t launch(ProductArgs &p, const void *qx, long long qx_ld, const void *qw, long long qw_ld, int width, int sms, cudaStream_t st, bool &mapped)
 {
     const int R = p.rows <= 16 ? 16 : p.rows <= 32 ? 32 : p.rows <= 64 ? 64 : 128;
-    const bool many = p.rows > 128;
+    // Pairs of CTAs from 64 tiles of 128 x 128 on.  us, few rows / pairs: 47 tiles (128 x 6000 x 1500) 11.1 / 11.9, 48 (700 x 1000 x 1500)
+    // 11.2 / 12.5, 64 (1000 x 1000 x 1500) 13.0 / 12.6, 94 (160 x 6000 x 1500) 14.1 / 11.9, 96 (400 x 3000 x 6000) 28.5 / 28.2, 192 (1000 x 3000
+    // x 6000) 49 / 30
+    const bool many = p.rows > 128 && (p.rows + 127ll) / 128 * ((p.outs + 127ll) / 128) >= 64;
     CUtensorMap mw, mx;
     mapped = encode_tmap_2d(&mw, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, qw, p.outs, width, qw_ld, kTileOuts) &&
-             encode_tmap_2d(&mx, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, qx, p.rows, width, qx_ld, R);
+             encode_tmap_2d(&mx, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, qx, p.rows, width, qx_ld, many ? 128 : R);
     if (!mapped) return cudaErrorInvalidValue;
     if (many) return launch_many<T>(p, mw, mx, sms, st);
     if (R == 16) return launch_few<T, 16>(p, mw, mx, sms, st);

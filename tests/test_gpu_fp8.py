@@ -70,7 +70,9 @@ def test_quantize_leaves_what_lies_between_rows():
 # every tile of rows, tiles and blocks that end anywhere, split and whole sums
 PRODUCTS = [(1, 1, 1), (1, 3, 16), (2, 128, 128), (3, 129, 127), (16, 130, 129), (17, 100, 300), (32, 256, 1500), (33, 257, 1501), (50, 6000, 1500), (64, 90, 2000),
             (65, 400, 96), (100, 300, 4100), (128, 128, 640), (129, 1000, 900), (257, 511, 1313), (300, 260, 33), (700, 3000, 1500), (1000, 2050, 520),
-            (2049, 1500, 200), (1, 6000, 1500), (4, 8192, 8192)]
+            (2049, 1500, 200), (1, 6000, 1500), (4, 8192, 8192),
+            # many tiles: pairs of CTAs, tiles, blocks and rows of the output that end anywhere, more blocks than are staged at once
+            (300, 4000, 129), (1030, 1100, 260), (520, 2051, 1500), (9000, 1, 40), (8300, 3, 257), (4000, 513, 64), (1500, 900, 2200), (700, 3001, 4200)]
 
 
 def operands(rows, outs, width, seed=0):
@@ -117,7 +119,7 @@ def test_random_sizes():
 
 def test_whole_numbers_are_exact():
     """Small whole numbers with scales of one: every sum is exact in 32 bits."""
-    for rows, outs, width in ((7, 300, 1000), (200, 300, 1000), (1024, 512, 777)):
+    for rows, outs, width in ((7, 300, 1000), (200, 300, 1000), (1024, 1100, 777)):
         g = torch.Generator(device="cuda").manual_seed(rows)
         x = torch.randint(-4, 5, (rows, width), generator=g, device="cuda").float()
         w = torch.randint(-4, 5, (outs, width), generator=g, device="cuda").float()
@@ -129,7 +131,7 @@ def test_whole_numbers_are_exact():
         assert torch.equal(y.double(), x.double() @ w.double().t())
 
 
-@pytest.mark.parametrize("rows", (3, 40, 300))
+@pytest.mark.parametrize("rows", (3, 40, 300, 4100))
 def test_nan_stays_in_its_row(rows):
     qx, sx, qw, sw, _ = operands(rows, 200, 300, 1)
     want = pkg.fp8_product(qx, sx, qw, sw)
@@ -145,7 +147,7 @@ def test_nan_stays_in_its_row(rows):
     assert torch.equal(y[:, :128], want[:, :128]) and not y[:, 128:].isfinite().any()
 
 
-@pytest.mark.parametrize("rows", (1, 20, 70, 500))
+@pytest.mark.parametrize("rows", (1, 20, 70, 500, 4400))
 @pytest.mark.parametrize("dtype", ("bf16", "fp32"))
 def test_rows_and_columns_beside_the_output_are_left(rows, dtype):
     qx, sx, qw, sw, bias = operands(rows, 131, 200, 2)
