@@ -519,7 +519,7 @@ cudaError_t by_vector(LinrecArgs &p, bool backward, int sms, cudaStream_t st)
     matrix(p.hT, 0, 0, 4);
     matrix(p.states, 0, 0, 4);
     int wide_v;
-    if (linrec_wide_serves(p, v, backward, sms, wide_v)) return launch_linrec_wide(p, wide_v, sizeof(T) == 2, backward, st);
+    if (linrec_wide_serves(p, v, sizeof(T) == 2, backward, sms, wide_v)) return launch_linrec_wide(p, wide_v, sizeof(T) == 2, backward, st);
     constexpr int kMost = 8 / sizeof(T);
     if (v >= kMost) return by_gate<T, kMost>(p, backward, sms, st);
     return v == 2 ? by_gate<T, 2>(p, backward, sms, st) : by_gate<T, 1>(p, backward, sms, st);

@@ -208,7 +208,7 @@ __device__ __forceinline__ int count_steps(long long i0, int last)
 // The kernels for many channels, and for chunks of time (linrec_wide.cu); a vector has v channels.
 // How many chunks a call is cut into, and their length (a multiple of 64): the same for a call's workspace and its launch.
 int linrec_chunks(int T, int B, int D, int &chunk_len);
-bool linrec_wide_serves(const LinrecArgs &p, int v, bool backward, int sms, int &wide_v);
+bool linrec_wide_serves(const LinrecArgs &p, int v, bool bf16, bool backward, int sms, int &wide_v);
 cudaError_t launch_linrec_wide(LinrecArgs &p, int v, bool bf16, bool backward, cudaStream_t st);
 
 }  // namespace lstm

@@ -14,19 +14,20 @@
 #include "../../include/lstm_b200.h"
 #include "linrec_parts.cuh"
 
+#include <algorithm>
 #include <type_traits>
 
 namespace lstm {
 namespace {
 
 // Steps of a warp's span, threads of a CTA, CTAs of an SM, and where inputs wait, for vectors of V channels.
-// Vectors of four lie in shared memory two spans ahead (of bf16 in registers: 2048 x 32 x 1500 151 us instead of 109); narrower ones wait
-// in registers (4096 x 8 x 1502 of fp32 in shared memory: 173 us instead of 113).
+// Four bf16 lie in shared memory two spans ahead (in registers: 2048 x 32 x 1500 151 us instead of 109); two or one wait in registers
+// (4096 x 8 x 1502 of fp32 in shared memory: 173 us instead of 113).  Four fp32 are not served: 16384 x 1500 135 us, with two 90.
 template <typename T, int V, bool BACK> struct Shape;
 template <typename T> struct Shape<T, 4, false> { static constexpr int kSteps = 4, kThreads = 128, kResident = 5, kDepth = 2; };
 template <typename T> struct Shape<T, 2, false> { static constexpr int kSteps = 8, kThreads = 256, kResident = 2, kDepth = 0; };
 template <typename T> struct Shape<T, 1, false> { static constexpr int kSteps = 16, kThreads = 128, kResident = 4, kDepth = 0; };
-template <typename T> struct Shape<T, 4, true> { static constexpr int kSteps = 4, kThreads = 128, kResident = 4, kDepth = sizeof(T) == 2 ? 2 : 1; };
+template <typename T> struct Shape<T, 4, true> { static constexpr int kSteps = 4, kThreads = 128, kResident = 4, kDepth = 2; };
 template <typename T> struct Shape<T, 2, true> { static constexpr int kSteps = 4, kThreads = 256, kResident = 2, kDepth = 0; };
 template <typename T> struct Shape<T, 1, true> { static constexpr int kSteps = 8, kThreads = 128, kResident = 4, kDepth = 0; };
 
@@ -467,7 +468,8 @@ cudaError_t launch(LinrecArgs &p, bool backward, cudaStream_t st)
 template <typename T>
 cudaError_t by_vector(LinrecArgs &p, int v, bool backward, cudaStream_t st)
 {
-    if (v == 4) return p.gate ? launch<T, 4, true>(p, backward, st) : launch<T, 4, false>(p, backward, st);
+    if constexpr (sizeof(T) == 2)
+        if (v == 4) return p.gate ? launch<T, 4, true>(p, backward, st) : launch<T, 4, false>(p, backward, st);
     if (v == 2) return p.gate ? launch<T, 2, true>(p, backward, st) : launch<T, 2, false>(p, backward, st);
     return p.gate ? launch<T, 1, true>(p, backward, st) : launch<T, 1, false>(p, backward, st);
 }
@@ -477,26 +479,28 @@ cudaError_t by_vector(LinrecArgs &p, int v, bool backward, cudaStream_t st)
 // Chunks pay where channels alone do not fill the chip and the work is large enough for a second launch and a second reading, most of
 // which comes from L2 up to some ten million elements.  us, cluster of CTAs (linrec.cu) / chunks: 65536 x 1 x 1500 of bf16 261 / 200,
 // backward 529 / 320; 16384 x 1 x 1500 69 / 59; 4096 x 4 x 1000 52 / 41; 65536 x 1 x 256 102 / 48; 4096 x 1 x 1500 20 / 21.
-// As many chunks as make some 48000 channels side by side, and no more than 64: each has to run through the maps of those before it.
+// As many chunks as make some 75000 channels side by side, just under what is resident at once (65536 x 1500: 36000 228 us, 48000 200, 93000
+// 194, 120000 217; backward 342, 320, 336, 340, and 72000 295), and no more than 64: each has to run through the maps of those before it.
 int linrec_chunks(int T, int B, int D, int &chunk_len)
 {
     chunk_len = T;
     const long long channels = (long long)B * D;
-    if (channels > 11000 || channels * T < 8000000 || T < 512) return 1;
-    const int want = (int)(48000 / channels < 2 ? 2 : 48000 / channels > 64 ? 64 : 48000 / channels);
+    // from here on vectors of two channels, or of one, make more than one CTA an SM by themselves (linrec_wide_serves)
+    if (channels > (D % 2 ? 5600 : 11000) || channels * T < 8000000 || T < 512) return 1;
+    const int want = (int)std::min(std::max(75000 / channels, 2ll), 64ll);
     const long long len = (((long long)T + want - 1) / want + 63) / 64 * 64;
     chunk_len = (int)len;
     return (int)((T + len - 1) / len);
 }
 
 // Without chunks: where vectors of four make two CTAs an SM, else with vectors of two where those make more than one.
-bool linrec_wide_serves(const LinrecArgs &p, int v, bool backward, int sms, int &wide_v)
+bool linrec_wide_serves(const LinrecArgs &p, int v, bool bf16, bool backward, int sms, int &wide_v)
 {
     const long long channels = (long long)p.chunks * p.B * p.D;
     auto groups = [&](int n) { return (channels / n + 31) / 32; };
-    wide_v = v;
+    wide_v = bf16 ? v : std::min(v, 2);
     if (p.T <= kShort && !backward) return true;
-    if (v == 4 && groups(4) < 2 * sms) wide_v = 2;
+    if (wide_v == 4 && groups(4) < 2 * sms) wide_v = 2;
     return p.chunks > 1 || groups(wide_v) * 5 >= 6ll * sms;
 }
 

@@ -70,7 +70,7 @@ __global__ void __launch_bounds__(ALONE ? 128 : NS == 2 ? 256 : 512, ALONE ? 12 
         sum = 0.0f;
         for (int i = 0; i < warps; ++i) sum += s[i];
     }
-    const float rstd = rsqrtf(sum / (float)p.width + p.eps);
+    const float rstd = __frsqrt_rn(sum / (float)p.width + p.eps);
 #pragma unroll
     for (int j = 0; j < NS; ++j) {
         const int c0 = (first + j * warps) * kStrip;
@@ -172,7 +172,7 @@ __global__ void __launch_bounds__(NS == 4 ? 512 : 256) rms_norm_backward_kernel(
             rr = ry = 0.0f;
             for (int i = 0; i < warps; ++i) { rr += s[turn][i].x; ry += s[turn][i].y; }
         }
-        const float rstd = rsqrtf(rr * each + p.eps);
+        const float rstd = __frsqrt_rn(rr * each + p.eps);
         const float mean = ry * each * rstd * rstd;
 #pragma unroll
         for (int j = 0; j < NS; ++j) {
