@@ -169,6 +169,14 @@ struct Joiner {
     }
 };
 
+// the values have been loaded when a thread gets past here
+template <int V>
+__device__ __forceinline__ void arrived(float (&v)[V])
+{
+#pragma unroll
+    for (int i = 0; i < V; ++i) asm volatile("mov.f32 %0, %0;" : "+f"(v[i])::"memory");
+}
+
 // What a thread works on
 template <int V>
 struct Place {
@@ -228,6 +236,7 @@ __global__ void __launch_bounds__(kThreads, 4) linrec_forward_kernel(const __gri
     float carry[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) carry[v] = at.live && p.h0 ? p.h0[at.bd + v] : 0.0f;
+    arrived<V>(carry);                  // another thread may write the final state over it
     joiner.ready();
     for (long long base = 0; base < p.T; base += span, i0 += span) {
         const int n = Place<V>::count(i0, at.len);
@@ -342,6 +351,7 @@ __global__ void __launch_bounds__(kThreads, V == 4 ? 2 : 3) linrec_backward_kern
 #pragma unroll
     for (int v = 0; v < V; ++v) carry[v] = at.live && p.h0 ? p.h0[at.bd + v] : 0.0f;
     saved(i0, hs);
+    arrived<V>(carry);
     joiner.ready();
     for (long long base = 0; base < nspan * kSteps; base += span, i0 -= span) {
         const int n = Place<V>::count(i0, at.len);
@@ -543,11 +553,13 @@ int check(const void *a, const void *x, int T, int B, int D, int dtype, int flag
     return LSTM_OK;
 }
 
+long long linrec_workspace(int chunks, int B, int D) { return chunks > 1 ? (2ll * chunks + 1) * B * D : 0; }
+
 int take_workspace(LinrecArgs &p, float *workspace, long long floats, const Failure &fail)
 {
     p.chunks = linrec_chunks(p.T, p.B, p.D, p.chunk_len);
     p.maps = workspace;
-    if (p.chunks > 1 && (!workspace || !aligned_to(workspace, 4) || floats < 2ll * p.chunks * p.B * p.D))
+    if (p.chunks > 1 && (!workspace || !aligned_to(workspace, 4) || floats < linrec_workspace(p.chunks, p.B, p.D)))
         return fail(LSTM_ERR_INVALID, "bad argument: the workspace is smaller than lstm_linear_recurrence_workspace says");
     return LSTM_OK;
 }
@@ -566,7 +578,7 @@ long long lstm_linear_recurrence_workspace(int T, int B, int D)
     if (T < 0 || B < 0 || D < 1) return -1;
     int chunk_len = 0;
     const int chunks = linrec_chunks(T, B, D, chunk_len);
-    return chunks > 1 ? 2ll * chunks * B * D : 0;
+    return linrec_workspace(chunks, B, D);
 }
 
 int lstm_linear_recurrence(const void *a, long long a_t, long long a_b, const void *x, long long x_t, long long x_b, const float *h0,

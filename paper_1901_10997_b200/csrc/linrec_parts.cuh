@@ -12,7 +12,7 @@ struct LinrecArgs {
     int T, B, D, nvec;          // vectors of channels per sequence
     int gate, reverse, csize;
     int chunks, chunk_len;      // time cut into chunks that run side by side (linrec_wide.cu): T = chunks * chunk_len or less
-    float *maps;                // [2][chunks][B][D], where there is more than one
+    float *maps;                // [2][chunks][B][D] and the initial carries [B][D], where there is more than one
     void *h;                    // backward: dx
     long long h_t, h_b;
     float *hT;                  // [B][D]; backward: dh0

@@ -70,12 +70,13 @@ struct Channels {
     }
 };
 
-// The carry of a thread's channel in front of its chunk: the initial one behind the maps of the chunks on the way.
+// The carry of a thread's channel in front of its chunk: the initial one behind the maps of the chunks on the way.  With several chunks the
+// first kernel has copied the initial ones behind the maps: the last chunk may write the final state over them while others begin.
 __device__ __forceinline__ float carry_before(const LinrecArgs &p, long long own, int chunk, bool backward)
 {
     if (own < 0) return 0.0f;
-    float carry = p.h0 ? p.h0[own] : 0.0f;
     const long long BD = (long long)p.B * p.D, plane = p.chunks * BD;
+    float carry = p.chunks > 1 ? p.maps[2 * plane + own] : p.h0 ? p.h0[own] : 0.0f;
     const int way = backward ? p.chunks - 1 - chunk : chunk;
 #pragma unroll 8
     for (int i = 0; i < way; ++i) {
@@ -157,6 +158,7 @@ __global__ void __launch_bounds__(128, 5) linrec_chunk_maps_kernel(const __grid_
             h = fmaf(mapA[w][threadIdx.x], h, mapH[w][threadIdx.x]);
             a = held<V, GATE>(a * mapA[w][threadIdx.x]);
         }
+        if (at.own_chunk == 0) p.maps[2ll * p.chunks * at.BD + at.own] = p.h0 ? p.h0[at.own] : 0.0f;
         p.maps[at.own_map] = a;
         p.maps[(long long)p.chunks * at.BD + at.own_map] = h;
     }
@@ -229,7 +231,7 @@ __global__ void __launch_bounds__(Shape<T, V, false>::kThreads, Shape<T, V, fals
                 carry = fmaf(a[w], carry, h[w]);
             }
         }
-        __syncthreads();            // maps are written again behind the next round's first barrier, by when `front` has been read
+        __syncthreads();            // from here the maps may be written again; `front` is behind the next round's first barrier, when all have read it
         const Vec<float, V> begin = load_vec<float, V>(&front[warp][lane * V]);
         float h[V];
 #pragma unroll

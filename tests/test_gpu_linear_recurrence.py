@@ -214,6 +214,26 @@ def test_state_in_place_and_missing_state(T):
     assert all(torch.equal(p, q) for p, q in zip(zero[:2], pkg.linear_recurrence(a, x)[:2]))
 
 
+@pytest.mark.parametrize("T, B, D", ((4100, 2, 1000), (300, 40, 602), (600, 1, 64)))
+def test_states_and_their_gradients_in_place(T, B, D):
+    """The final state over the initial one where many CTAs read it: chunks of time, many channels, a cluster."""
+    a, x, h0, _, dh, dhT = make(T, B, D, "bf16", True, False, "fused", 13)
+    want = pkg.linear_recurrence(a, x, h0, save=True)
+    grads = pkg.linear_recurrence_backward(a, x, want[2], dh, dhT)
+    for _ in range(5):
+        state = h0.clone()
+        h, _, _ = pkg.linear_recurrence(a, x, state, state=state)
+        assert torch.equal(h, want[0]) and torch.equal(state, want[1])
+        need = pkg.lstm_linear_recurrence_workspace(T, B, D)
+        work, g, da, dx = torch.empty(max(need, 1), device="cuda"), dhT.clone(), torch.empty_like(h), torch.empty_like(h)
+        rc, why = pkg.lstm_linear_recurrence_backward(a.data_ptr(), a.stride(0), a.stride(1), x.data_ptr(), x.stride(0), x.stride(1), want[2].data_ptr(),
+                                                      dh.data_ptr(), dh.stride(0), dh.stride(1), g.data_ptr(), 0, T, B, D, pkg.LSTM_BF16, pkg.LSTM_LINREC_GATE,
+                                                      da.data_ptr(), B * D, D, dx.data_ptr(), B * D, D, g.data_ptr(), work.data_ptr(), need,
+                                                      torch.cuda.current_stream().cuda_stream)
+        assert rc == pkg.LSTM_OK, why
+        assert all(torch.equal(p, q) for p, q in zip((da, dx, g), grads))
+
+
 def test_chunks_carry_the_state():
     T, B, D = 500, 2, 40
     a, x, h0, *_ = make(T, B, D, "fp32", True, False, "fused", 8)

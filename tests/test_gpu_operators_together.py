@@ -115,3 +115,35 @@ def test_a_training_step():
     # sums of up to 135 rows and 128 columns and of the recurrence's memory, all in 32 bits: some 1000 roundings of U against the whole
     for got, wanted in zip((dx, dw, dW, dh0), want):
         assert float((got.double() - wanted).norm() / wanted.norm()) <= 1000 * ref.U
+
+
+FIRST = """
+import torch, paper_1901_10997_b200 as pkg
+n = lambda *s: torch.randn(s, device="cuda")
+x, w, z, z2, dh = n(30, 200).bfloat16(), n(200), n(90, 2, 96).bfloat16(), n(9000, 1, 1000), n(90, 2, 96).bfloat16()
+wide, m, states = n(40, 30, 900).bfloat16(), n(400, 200).bfloat16(), n(6, 2, 96)
+many = n(9000, 200).bfloat16()
+torch.cuda.synchronize()
+g = torch.cuda.CUDAGraph()
+def run():
+    q, s, r = pkg.rms_norm_fp8(x, w, x)
+    qw, sw = pkg.fp8_quantize(m, block_rows=128)
+    return [pkg.fp8_product(q, s, qw, sw), pkg.fp8_product(*pkg.fp8_quantize(many), qw, sw), *pkg.rms_norm_backward(x, x, w), pkg.linear_recurrence(z, z)[0],
+            pkg.linear_recurrence(z2, z2)[0], pkg.linear_recurrence(wide, wide)[0], *pkg.linear_recurrence_backward(z, z, states, dh), s, r]
+with torch.cuda.graph(g):
+    out = run()
+g.replay()
+torch.cuda.synchronize()
+assert all(torch.equal(p, q) for p, q in zip(out, run()))
+print("same")
+"""
+
+
+def test_the_first_call_of_a_process_may_be_a_recorded_one():
+    import os
+    import subprocess
+    import sys
+    from pathlib import Path
+    root = Path(__file__).resolve().parent.parent
+    r = subprocess.run([sys.executable, "-c", FIRST], capture_output=True, text=True, timeout=300, cwd=str(root), env=dict(os.environ, PYTHONPATH=str(root)))
+    assert r.returncode == 0 and "same" in r.stdout, r.stderr[-2000:]
