@@ -22,6 +22,7 @@ struct ProductArgs {
     const float *sx, *sw, *bias;
     void *y;
     long long y_ld;
+    int stored;                       // y is written by tensor copies (its rows start and end on 16 bytes)
 };
 
 __device__ __forceinline__ void umma_e4m3(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate)
@@ -322,7 +323,8 @@ __device__ __forceinline__ void add_scaled(float &s0, float &s1, uint32_t v0, ui
 
 template <typename T>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
-fp8_many_rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x, const __grid_constant__ ProductArgs p)
+fp8_many_rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_y,
+                     const __grid_constant__ ProductArgs p)
 {
     extern __shared__ __align__(16) unsigned char smem_raw[];
     __shared__ __align__(8) unsigned long long full_bar[kPairStages], empty_bar[kPairStages], sums_full[4], sums_empty[4], scales_full[2], scales_empty[2];
@@ -354,7 +356,8 @@ fp8_many_rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem_base = tmem_base_s;
     volatile int *abort_flag = &abort_s;
-    float *staged = reinterpret_cast<float *>(smem_raw + (tiles - smem_u32(smem_raw)) + kPairStages * 2 * kHalfTile);
+    unsigned char *behind = smem_raw + (tiles - smem_u32(smem_raw)) + kPairStages * 2 * kHalfTile;       // a multiple of 1024 bytes
+    float *staged = reinterpret_cast<float *>(behind + 16 * kTurn * 4);
 
     if (warp >= 18) {
         // rows 64 (warp - 18) and on: lane = row of eight, word of four
@@ -439,7 +442,7 @@ fp8_many_rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
         // a half's 128 columns of tensor memory are 64 rows of w from each CTA
         const int quad = warp & 3, part = warp >> 2, col0 = (part & 1) * 128 + (part >> 1) * 64;
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;
-        uint32_t *turn = reinterpret_cast<uint32_t *>(staged + 2 * kScales) + warp * kTurn;
+        uint32_t *turn = reinterpret_cast<uint32_t *>(behind) + warp * (p.stored ? 32 * 32 : kTurn);
         T *y = (T *)p.y;
         constexpr int kWord = 4 / sizeof(T);                        // columns of a word
         // words that may be stored at once: two, one, or (rows of bf16 that start anywhere) half of one
@@ -499,7 +502,28 @@ fp8_many_rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
 #pragma unroll
                 for (int c = 0; c < kPairCols; ++c) sum[c] = __uint_as_float(0x7fffffffu);
             }
-            // a thread has a row, memory wants columns side by side: 32 x 32 words at a time change places within the warp
+            // A thread has a row, memory wants columns side by side: 32 rows of 128 bytes go through shared memory, from where a tensor
+            // copy takes them (and leaves out what lies outside of y) while the warp goes on ...
+            if (p.stored) {
+#pragma unroll
+                for (int c0 = 0; c0 < kPairCols; c0 += 32 * kWord) {
+                    if (n0 + c0 >= p.outs || m0 >= p.rows) break;
+                    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                    __syncwarp();
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)          // 16 bytes, in the swizzle's place
+                        *reinterpret_cast<Vec<T, 4 * kWord> *>(turn + lane * 32 + (j ^ (lane & 7)) * 4) = to_vec<T, 4 * kWord>(&sum[c0 + j * 4 * kWord]);
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) {
+                        asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];"
+                                     ::"l"(&map_y), "r"(n0 + c0), "r"(m0), "r"(smem_u32(turn)) : "memory");
+                        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                    }
+                }
+                continue;
+            }
+            // ... or, where rows start anywhere, 32 x 32 words at a time change places within the warp
             const int rows = min(32, p.rows - m0);
 #pragma unroll
             for (int c0 = 0; c0 < kPairCols; c0 += 32 * kWord) {
@@ -531,6 +555,8 @@ fp8_many_rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
                 }
             }
         }
+        if (p.stored && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+        __syncwarp();
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
@@ -544,6 +570,11 @@ fp8_many_rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
 template <typename T>
 cudaError_t launch_many(ProductArgs &p, const CUtensorMap &mw, const CUtensorMap &mx, int sms, cudaStream_t st)
 {
+    CUtensorMap my = mx;
+    const int es = (int)sizeof(T);
+    // (a row whose length is no multiple of 16 bytes would be written up to the next one)
+    p.stored = aligned_to(p.y, 16) && p.y_ld * es % 16 == 0 && (long long)p.outs * es % 16 == 0 && p.y_ld >= p.outs &&
+               encode_tmap_2d(&my, es == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, es, p.y, p.rows, p.outs, p.y_ld, 32);
     const void *fn = (const void *)fp8_many_rows_kernel<T>;
     static std::atomic<unsigned long long> prepared;
     const cudaError_t e = prepare_kernel(fn, prepared, kPairSmem + 1024, false);
@@ -555,7 +586,7 @@ cudaError_t launch_many(ProductArgs &p, const CUtensorMap &mw, const CUtensorMap
     cfg.blockDim = dim3(kPairThreads);
     cfg.dynamicSmemBytes = kPairSmem + 1024;
     cfg.stream = st;
-    void *args[] = {(void *)&mw, (void *)&mx, &p};
+    void *args[] = {(void *)&mw, (void *)&mx, (void *)&my, &p};
     return cudaLaunchKernelExC(&cfg, fn, args);
 }
 

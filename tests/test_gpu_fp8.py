@@ -149,11 +149,13 @@ def test_nan_stays_in_its_row(rows):
 
 @pytest.mark.parametrize("rows", (1, 20, 70, 500, 4400))
 @pytest.mark.parametrize("dtype", ("bf16", "fp32"))
-def test_rows_and_columns_beside_the_output_are_left(rows, dtype):
-    qx, sx, qw, sw, bias = operands(rows, 131, 200, 2)
+# rows that start anywhere, on 16 and on 4 bytes, and end anywhere or on 16 bytes
+@pytest.mark.parametrize("at, ld, outs", ((3, 140, 131), (16, 176, 131), (2, 142, 131), (16, 176, 136)))
+def test_rows_and_columns_beside_the_output_are_left(rows, dtype, at, ld, outs):
+    qx, sx, qw, sw, bias = operands(rows, outs, 200, 2)
     want = pkg.fp8_product(qx, sx, qw, sw, bias, dtype=ref.TYPES[dtype])
-    held = torch.full((rows + 2, 140), 5.0, dtype=ref.TYPES[dtype], device="cuda")
-    out = held[1:rows + 1, 3:134]
+    held = torch.full((rows + 2, ld), 5.0, dtype=ref.TYPES[dtype], device="cuda")
+    out = held[1:rows + 1, at:at + outs]
     assert pkg.fp8_product(qx, sx, qw, sw, bias, dtype=held.dtype, out=out) is out
     assert torch.equal(out, want)
     out.fill_(5.0)
