@@ -33,36 +33,6 @@ __device__ __forceinline__ float rcp_fast(float x)
 
 // f and 1 - f, both to full relative accuracy: with e = exp(-|u|) they are 1/(1+e) and e/(1+e), in the order that the sign says.
 // bf16 data: the hardware's exponential (error 2^-22 and |u| 2^-24) is far inside a rounding to 8 bits; fp32 data: expf.
-// d = a b + c and d = a b over the channels of a vector, two to an instruction
-template <int V>
-__device__ __forceinline__ void fma_vec(float (&d)[V], const float (&a)[V], const float (&b)[V], const float (&c)[V])
-{
-    if (V == 1) { d[0] = fmaf(a[0], b[0], c[0]); return; }
-#pragma unroll
-    for (int v = 0; v + 1 < V; v += 2)
-        asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\t"
-            "fma.rn.f32x2 x, x, y, z;\n\tmov.b64 {%0, %1}, x;\n\t}"
-            : "=f"(d[v]), "=f"(d[v + 1]) : "f"(a[v]), "f"(a[v + 1]), "f"(b[v]), "f"(b[v + 1]), "f"(c[v]), "f"(c[v + 1]));
-}
-template <int V>
-__device__ __forceinline__ void mul_vec(float (&d)[V], const float (&a)[V], const float (&b)[V])
-{
-    if (V == 1) { d[0] = a[0] * b[0]; return; }
-#pragma unroll
-    for (int v = 0; v + 1 < V; v += 2)
-        asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmul.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
-            : "=f"(d[v]), "=f"(d[v + 1]) : "f"(a[v]), "f"(a[v + 1]), "f"(b[v]), "f"(b[v + 1]));
-}
-template <int V>
-__device__ __forceinline__ void add_vec(float (&d)[V], const float (&a)[V], const float (&b)[V])
-{
-    if (V == 1) { d[0] = a[0] + b[0]; return; }
-#pragma unroll
-    for (int v = 0; v + 1 < V; v += 2)
-        asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tadd.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
-            : "=f"(d[v]), "=f"(d[v + 1]) : "f"(a[v]), "f"(a[v + 1]), "f"(b[v]), "f"(b[v + 1]));
-}
-
 // u -> f and w = 1 - f
 template <typename T, int V>
 __device__ __forceinline__ void gate_vec(const float (&u)[V], float (&f)[V], float (&w)[V])

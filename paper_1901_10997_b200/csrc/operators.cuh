@@ -129,6 +129,38 @@ __device__ __forceinline__ void store_raw(T *p, const Vec<T, V> &v)
 template <typename T, int V>
 __device__ __forceinline__ void store_vec(T *p, const float (&o)[V]) { store_raw<T, V>(p, to_vec<T, V>(o)); }
 
+// ---------------------------------------------------------------------------------------------------
+// fp32 arithmetic on V values, two to an instruction: d = a b + c, d = a b, d = a + b
+// ---------------------------------------------------------------------------------------------------
+template <int V>
+__device__ __forceinline__ void fma_vec(float (&d)[V], const float (&a)[V], const float (&b)[V], const float (&c)[V])
+{
+    if (V == 1) { d[0] = fmaf(a[0], b[0], c[0]); return; }
+#pragma unroll
+    for (int v = 0; v + 1 < V; v += 2)
+        asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\t"
+            "fma.rn.f32x2 x, x, y, z;\n\tmov.b64 {%0, %1}, x;\n\t}"
+            : "=f"(d[v]), "=f"(d[v + 1]) : "f"(a[v]), "f"(a[v + 1]), "f"(b[v]), "f"(b[v + 1]), "f"(c[v]), "f"(c[v + 1]));
+}
+template <int V>
+__device__ __forceinline__ void mul_vec(float (&d)[V], const float (&a)[V], const float (&b)[V])
+{
+    if (V == 1) { d[0] = a[0] * b[0]; return; }
+#pragma unroll
+    for (int v = 0; v + 1 < V; v += 2)
+        asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmul.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
+            : "=f"(d[v]), "=f"(d[v + 1]) : "f"(a[v]), "f"(a[v + 1]), "f"(b[v]), "f"(b[v + 1]));
+}
+template <int V>
+__device__ __forceinline__ void add_vec(float (&d)[V], const float (&a)[V], const float (&b)[V])
+{
+    if (V == 1) { d[0] = a[0] + b[0]; return; }
+#pragma unroll
+    for (int v = 0; v + 1 < V; v += 2)
+        asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tadd.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
+            : "=f"(d[v]), "=f"(d[v + 1]) : "f"(a[v]), "f"(a[v + 1]), "f"(b[v]), "f"(b[v + 1]));
+}
+
 inline bool known_type(int dtype) { return dtype == LSTM_F32 || dtype == LSTM_BF16; }
 inline int bytes_of(int dtype) { return dtype == LSTM_BF16 ? 2 : 4; }
 inline bool aligned_to(const void *p, int bytes) { return (uintptr_t)p % (unsigned)bytes == 0; }

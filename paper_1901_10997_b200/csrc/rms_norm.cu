@@ -23,13 +23,21 @@ struct NormArgs {
     float *scales;              // not NULL: y is e4m3
     void *r;
     long long r_ld;
+    float each;                 // 1 / width
 };
+
+// 1 / sqrt(v): the hardware's approximation and one Newton step; 0 gives infinity, infinity 0
+__device__ __forceinline__ float reciprocal_root(float v)
+{
+    const float y = rsqrtf(v), better = fmaf(0.5f * y, fmaf(-v * y, y, 1.0f), y);
+    return v > 0.0f && v < __int_as_float(0x7f800000) ? better : y;
+}
 
 // NS strips a warp.  Up to two strips, a warp has a row to itself and four stand in a CTA; wider rows have a CTA each, whose
 // warps meet once.  Few registers a thread and many CTAs: that, not the work of a thread, is what keeps the memory busy.
 constexpr int kNormWarps = 16;
 template <typename T, int V, int NS, bool ALONE>
-__global__ void __launch_bounds__(ALONE ? 128 : NS == 2 ? 256 : 512, ALONE ? 12 : NS == 2 ? 4 : 1) rms_norm_kernel(const __grid_constant__ NormArgs p)
+__global__ void __launch_bounds__(ALONE ? 128 : 512, ALONE ? 12 : NS == 2 ? 2 : 1) rms_norm_kernel(const __grid_constant__ NormArgs p)
 {
     __shared__ float s[kNormWarps];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -52,16 +60,18 @@ __global__ void __launch_bounds__(ALONE ? 128 : NS == 2 ? 256 : 512, ALONE ? 12 
             for (int i = 0; i < 8; ++i) r[j][i] = a[j][i];
         if (res) {
 #pragma unroll
-            for (int j = 0; j < NS; ++j)
+            for (int j = 0; j < NS; ++j) {
+                float add[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) r[j][i] += b[j][i];
+                for (int i = 0; i < 8; ++i) add[i] = b[j][i];
+                add_vec<8>(r[j], r[j], add);
+            }
         }
     }
-    float sum = 0.0f;
+    float part[8] = {};
 #pragma unroll
-    for (int j = 0; j < NS; ++j)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) sum = fmaf(r[j][i], r[j][i], sum);
+    for (int j = 0; j < NS; ++j) fma_vec<8>(part, r[j], r[j], part);
+    float sum = ((part[0] + part[1]) + (part[2] + part[3])) + ((part[4] + part[5]) + (part[6] + part[7]));
 #pragma unroll
     for (int o = 16; o > 0; o /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     if (!ALONE) {
@@ -70,7 +80,10 @@ __global__ void __launch_bounds__(ALONE ? 128 : NS == 2 ? 256 : 512, ALONE ? 12 
         sum = 0.0f;
         for (int i = 0; i < warps; ++i) sum += s[i];
     }
-    const float rstd = __frsqrt_rn(sum / (float)p.width + p.eps);
+    const float rstd = reciprocal_root(sum * p.each + p.eps);
+    float rs[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) rs[i] = rstd;
 #pragma unroll
     for (int j = 0; j < NS; ++j) {
         const int c0 = (first + j * warps) * kStrip;
@@ -79,8 +92,8 @@ __global__ void __launch_bounds__(ALONE ? 128 : NS == 2 ? 256 : 512, ALONE ? 12 
         if (p.r) store_strip<T, V>((T *)p.r + row * p.r_ld, c0, p.width, lane, r[j]);
         float w[8], y[8];
         load_strip<float, V>(p.w, c0, p.width, lane, w);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = r[j][i] * rstd * w[i];
+        mul_vec<8>(y, r[j], rs);
+        mul_vec<8>(y, y, w);
         if (!p.scales) {
             store_strip<T, V>((T *)p.y + row * p.y_ld, c0, p.width, lane, y);
             continue;
@@ -172,7 +185,7 @@ __global__ void __launch_bounds__(NS == 4 ? 512 : 256) rms_norm_backward_kernel(
             rr = ry = 0.0f;
             for (int i = 0; i < warps; ++i) { rr += s[turn][i].x; ry += s[turn][i].y; }
         }
-        const float rstd = __frsqrt_rn(rr * each + p.eps);
+        const float rstd = reciprocal_root(rr * each + p.eps);
         const float mean = ry * each * rstd * rstd;
 #pragma unroll
         for (int j = 0; j < NS; ++j) {
@@ -219,17 +232,17 @@ __global__ void __launch_bounds__(1024) rms_norm_join_kernel(const float *part, 
 // strips of a warp and warps of a CTA for a width: few strips a warp, and no idle one but in the last
 struct RowShape {
     int ns, warps;
-    explicit RowShape(int width)
+    RowShape(int width, bool backward)
     {
         const int strips = (width + kStrip - 1) / kStrip;
-        ns = strips <= 16 ? 2 : 4;
+        ns = strips <= (backward ? 16 : 32) ? 2 : 4;
         warps = (strips + ns - 1) / ns;
     }
 };
 template <typename T, int V>
 void launch_norm(const NormArgs &p, cudaStream_t st)
 {
-    const RowShape s(p.width);
+    const RowShape s(p.width, false);
     if (s.warps == 1) rms_norm_kernel<T, V, 2, true><<<(unsigned)((p.rows + 3ll) / 4), 128, 0, st>>>(p);
     else if (s.ns == 2) rms_norm_kernel<T, V, 2, false><<<p.rows, s.warps * 32, 0, st>>>(p);
     else rms_norm_kernel<T, V, 4, false><<<p.rows, s.warps * 32, 0, st>>>(p);
@@ -238,7 +251,7 @@ void launch_norm(const NormArgs &p, cudaStream_t st)
 // the most CTAs of the backward kernel, each of which leaves a row of partial sums: 16 warps an SM
 int parts_of(int rows, int width, int sms)
 {
-    const RowShape s(width);
+    const RowShape s(width, true);
     const int resident = s.warps >= 16 ? 1 : 16 / s.warps;
     return rows < sms * resident ? rows : sms * resident;
 }
@@ -259,7 +272,7 @@ int launch_back_shape(const NormBackArgs &p, int warps, int parts, int sms, cuda
 template <typename T, int V>
 int launch_back(const NormBackArgs &p, int parts, int sms, cudaStream_t st)
 {
-    const RowShape s(p.width);
+    const RowShape s(p.width, true);
     return s.ns == 2 ? launch_back_shape<T, V, 2>(p, s.warps, parts, sms, st) : launch_back_shape<T, V, 4>(p, s.warps, parts, sms, st);
 }
 
@@ -311,7 +324,7 @@ int lstm_rms_norm(const void *x, long long x_ld, const void *residual, long long
     al.matrix(r, r_ld, es);
     al.matrix(w, 0, 4);
     if (!scales) al.matrix(y, y_ld, es);
-    NormArgs p = {x, residual, x_ld, residual_ld, w, eps, rows, width, y, y_ld, scales, r, r_ld};
+    NormArgs p = {x, residual, x_ld, residual_ld, w, eps, rows, width, y, y_ld, scales, r, r_ld, 1.0f / (float)width};
     by_type<Forward>(dtype, al.v, p, (cudaStream_t)cuda_stream);
     const cudaError_t e = cudaGetLastError();
     return e == cudaSuccess ? LSTM_OK : fail.cuda(e);

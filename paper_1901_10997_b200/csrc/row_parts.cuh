@@ -76,10 +76,13 @@ __device__ __forceinline__ float per_scale(float scale)
     return y;
 }
 // (scale: at most the largest finite number; beside an infinite one, finite values are zero)
-__device__ __forceinline__ float in_units(float x, float scale, float per)
+__device__ __forceinline__ void in_units(float (&y)[4], const float (&x)[4], float scale, float per)
 {
-    const float t = x * per;
-    return fmaf(fmaf(-t, scale, x), per, t);
+    const float p[4] = {per, per, per, per}, s[4] = {-scale, -scale, -scale, -scale};
+    float t[4], left[4];
+    mul_vec<4>(t, x, p);
+    fma_vec<4>(left, t, s, x);
+    fma_vec<4>(y, left, p, t);
 }
 // two values as e4m3, the nearest, at most 448 in magnitude
 __device__ __forceinline__ unsigned to_e4m3x2(float a, float b)
@@ -116,9 +119,11 @@ __device__ __forceinline__ void store_strip_e4m3(uint8_t *row, int c0, int width
     const float per0 = per_scale(s0), per1 = V == 8 ? per0 : per_scale(s1);
     const bool whole = c0 + kStrip <= width;
     const float f0 = fminf(s0, 3.4028235e38f), f1 = fminf(s1, 3.4028235e38f);
-    float y[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = V == 8 || i < 4 ? in_units(x[i], f0, per0) : in_units(x[i], f1, per1);
+    const float lo[4] = {x[0], x[1], x[2], x[3]}, hi[4] = {x[4], x[5], x[6], x[7]};
+    float a[4], b[4];
+    in_units(a, lo, f0, per0);
+    in_units(b, hi, V == 8 ? f0 : f1, per1);
+    const float y[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
 #pragma unroll
     for (int q = 0; q < 8 / V; ++q) {
         const int c = c0 + strip_col<V>(q, lane);
