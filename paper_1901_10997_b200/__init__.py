@@ -18,5 +18,14 @@ from .binding import (LSTM, HLSTM, LstmError, hlstm_create, lib_path, load_libra
                       LSTM_PROBE_NO_PRODUCTS, LSTM_PROBE_NO_GATES, LSTM_PROBE_NO_EXCHANGE, LSTM_PROBE_WHOLE_STEP,
                       LSTM_RAN_NONE, LSTM_RAN_SHARED, LSTM_RAN_REGISTERS, LSTM_RAN_ONE, LSTM_RAN_WAVE, LSTM_RAN_BATCHED, LSTM_RAN_SPARSE,
                       LSTM_RAN_F32, LSTM_RAN_STEP, LSTM_RAN_HLSTM_ROWS, LSTM_RAN_HLSTM_TILES, RECUR_KERNELS)
-from .operators import (fp8_product, fp8_quantize, linear_recurrence, linear_recurrence_backward, rms_norm,  # noqa: F401
-                        rms_norm_backward, rms_norm_fp8)
+
+_ON_TENSORS = ("linear_recurrence", "linear_recurrence_backward", "rms_norm", "rms_norm_fp8", "rms_norm_backward", "fp8_quantize", "fp8_product")
+
+
+def __getattr__(name):
+    """The operators on torch tensors; torch is imported with the first of them."""
+    if name in _ON_TENSORS:
+        from . import operators
+        globals().update({n: getattr(operators, n) for n in _ON_TENSORS})
+        return globals()[name]
+    raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

@@ -55,6 +55,12 @@ __device__ __forceinline__ void tmem_arrived(uint32_t (&v)[16])
                    "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15])::"memory");
 }
 
+// A fetching thread that gives up lets its copies in flight land (microseconds; this is milliseconds) before the CTA's memory goes.
+__device__ __forceinline__ void let_copies_land()
+{
+    for (int i = 0; i < 4; ++i) __nanosleep(1000000);
+}
+
 __device__ __forceinline__ uint32_t rank_in_cluster()
 {
     uint32_t r;
@@ -77,6 +83,8 @@ __device__ __forceinline__ void cluster_sync()
 // Few rows of x: bound by the bytes of w.  128 rows of w are the M operand, R rows of x the N operand, and the blocks of columns
 // are split over a cluster of up to eight CTAs so that all SMs read; their sums meet in distributed shared memory, in one order.
 // Warps 0-3 read the accumulators back (quadrant = warp), warp 4 fetches, warp 5 multiplies.
+// One row x 6000 x 1500 takes 5.3 us, 16 rows 6.0, one row x 8192 x 8192 (10.3 us of bytes) 15.5: a launch and its fill (tensor memory, maps,
+// first bytes) are 3 to 4 us of each.
 // ---------------------------------------------------------------------------------------------------
 constexpr int kFewThreads = 192;
 constexpr int kFewSmem = 108 * 1024;
@@ -124,7 +132,7 @@ fp8_few_rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
             int s = 0;
             uint32_t ph = 0;
             for (int i = 0; i < nj; ++i) {
-                if (!mbar_wait(smem_u32(&empty_bar[s]), ph ^ 1u, abort_flag)) break;
+                if (!mbar_wait(smem_u32(&empty_bar[s]), ph ^ 1u, abort_flag)) { let_copies_land(); break; }
                 const uint32_t fb = smem_u32(&full_bar[s]), at = tiles + (uint32_t)s * kStage;
                 mbar_expect_tx(fb, kStage);
                 tma_load_2d(at, &map_w, fb, (j0 + i) * kBlockK, n_tile * kTileOuts);
@@ -279,6 +287,9 @@ cudaError_t launch_few(ProductArgs &p, const CUtensorMap &mw, const CUtensorMap 
 // Warps 0-15 read the accumulators back (quadrant = warp % 4, 64 columns each), warp 16 fetches, warp 17 of the first
 // CTA multiplies for both, warps 18 and 19 bring the scales of the rows of x, which lie a row's length apart, 16 blocks at a time into
 // shared memory (each reading warp on its own would touch 32 lines a block).
+// 25600 x 6400 x 1600 in 284 us: 1850 TFLOP/s, the tensor pipe 49 % active.  Of those 206 are operands and products (without reading
+// back), 50 the reading back, the rest the tiles' ends.  Steps: eight reading warps with 128 sums each 704 us, 16 with 64 410, scales staged and
+// results turned in shared memory 306, tensor copies of the results 284.
 // ---------------------------------------------------------------------------------------------------
 constexpr int kPairRows = 256, kPairOuts = 256;
 constexpr int kPairThreads = 640;
@@ -395,7 +406,7 @@ fp8_many_rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
             for (long long tile = pair; tile < all && ok; tile += pairs) {
                 const int m0 = (int)(tile / n_tiles) * kPairRows + rank * 128, n0 = (int)(tile % n_tiles) * kPairOuts + rank * 128;
                 for (int j = 0; j < p.blocks; ++j) {
-                    if (!(ok = mbar_wait(smem_u32(&empty_bar[s]), ph ^ 1u, abort_flag))) break;
+                    if (!(ok = mbar_wait(smem_u32(&empty_bar[s]), ph ^ 1u, abort_flag))) { let_copies_land(); break; }
                     const uint32_t at = tiles + (uint32_t)s * 2 * kHalfTile, fb = at_rank(smem_u32(&full_bar[s]), 0);
                     if (rank == 0) mbar_expect_tx(smem_u32(&full_bar[s]), 4 * kHalfTile);      // both CTAs' tiles
                     tma_load_2d_pair(at, &map_x, fb, j * kBlockK, m0);

