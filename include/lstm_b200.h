@@ -462,6 +462,7 @@ LSTM_API int lstm_rms_norm_backward(const void *dy, long long dy_ld, const void 
  * activations; scales [rows, ceil(width / 128)]) or to a block of 128 x 128 (block_rows = 128, weights;
  * scales [ceil(rows / 128), ceil(width / 128)]); the last block of a row or column may be smaller.
  *     scale = max |x| / 448 over the block, at least the smallest normal number;   q = x / scale, the nearest, ties to even
+ * (the quotient by the unrounded scale, as fp32 has it: ties are those of 448 x / max |x|).
  * A block that holds an infinity or a NaN gets that as its scale.  q rows start on 16 bytes (q and q_ld are multiples of
  * 16); the bytes between width and q_ld are left as they are.
  */

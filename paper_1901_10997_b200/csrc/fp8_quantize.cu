@@ -1,7 +1,6 @@
 // 8-bit values (e4m3) with a scale for each 128 columns of a row, or for each 128 x 128 block: the largest magnitude of a block
 // becomes 448, q = x / scale rounded to the nearest.  Bound by memory; every element is read once and stays in registers between
-// the maximum and the rounding.  Rows: 25600 x 1312 of bf16 in 24 us, 0.64 of the copy rate, 77 % of the issue slots taken (the quotient's
-// correction, maxima, conversions: 19 instructions an element); blocks: 5000 x 6000 in 20 us, 0.69.
+// the maximum and the rounding.  Rows: 25600 x 1312 of bf16 in 23.8 us, 0.66 of the copy rate; blocks: 5000 x 6000 in 20 us, 0.69.
 #include "../../include/lstm_b200.h"
 #include "row_parts.cuh"
 
@@ -42,7 +41,8 @@ __global__ void __launch_bounds__(256) fp8_quantize_rows_kernel(const __grid_con
         unsigned top[2];
         strip_magnitudes<V>(x, lane, top);
         const float s0 = block_scale(top[0]), s1 = V == 8 ? s0 : block_scale(top[1]);
-        store_strip_e4m3<V>(p.q + row * p.q_ld, c0, p.width, lane, x, s0, s1);
+        const Units u0 = block_units(top[0], s0), u1 = V == 8 ? u0 : block_units(top[1], s1);
+        store_strip_e4m3<V>(p.q + row * p.q_ld, c0, p.width, lane, x, u0, u1);
         float *out = p.scales + row * blocks + c0 / 128;
         if (lane == 0) out[0] = s0;
         if (lane == 16 && c0 + 128 < p.width) out[1] = s1;
@@ -85,15 +85,17 @@ __global__ void __launch_bounds__(128 / ROWS * 32, ROWS == 8 ? 2 : 1) fp8_quanti
     __syncthreads();
     top[0] = lane < kWarps ? tops[lane][0] : 0u;
     top[1] = lane < kWarps ? tops[lane][1] : 0u;
-    const float s0 = block_scale(__reduce_max_sync(0xffffffffu, top[0])), s1 = block_scale(__reduce_max_sync(0xffffffffu, top[1]));
-    const float mine = V == 8 && lane >= 16 ? s1 : s0;
+    top[0] = __reduce_max_sync(0xffffffffu, top[0]);
+    top[1] = __reduce_max_sync(0xffffffffu, top[1]);
+    const float s0 = block_scale(top[0]), s1 = block_scale(top[1]);
+    const Units u0 = block_units(top[0], s0), u1 = block_units(top[1], s1), mine = V == 8 && lane >= 16 ? u1 : u0;
 #pragma unroll
     for (int j = 0; j < ROWS; ++j) {
         if (j >= rows) break;
         float x[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] = raw[j][i];
-        store_strip_e4m3<V>(p.q + (r0 + j) * p.q_ld, c0, p.width, lane, x, mine, s1);
+        store_strip_e4m3<V>(p.q + (r0 + j) * p.q_ld, c0, p.width, lane, x, mine, u1);
     }
     if (threadIdx.x == 0) {
         float *out = p.scales + (long long)blockIdx.y * blocks + c0 / 128;

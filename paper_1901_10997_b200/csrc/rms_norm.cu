@@ -103,7 +103,8 @@ __global__ void __launch_bounds__(ALONE ? 128 : 512, ALONE ? 12 : NS == 2 ? 2 : 
         unsigned top[2];
         strip_magnitudes<V>(y, lane, top);
         const float s0 = block_scale(top[0]), s1 = V == 8 ? s0 : block_scale(top[1]);
-        store_strip_e4m3<V>((uint8_t *)p.y + row * p.y_ld, c0, p.width, lane, y, s0, s1);
+        const Units u0 = block_units(top[0], s0), u1 = V == 8 ? u0 : block_units(top[1], s1);
+        store_strip_e4m3<V>((uint8_t *)p.y + row * p.y_ld, c0, p.width, lane, y, u0, u1);
         const int blocks = (p.width + 127) / 128;
         float *out = p.scales + row * blocks + c0 / 128;
         if (lane == 0) out[0] = s0;

@@ -58,31 +58,33 @@ __device__ __forceinline__ void store_strip(T *row, int c0, int width, int lane,
 // |x| as an integer of the same order, in which NaN is above infinity
 __device__ __forceinline__ unsigned magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
 
-// The scale of a block from its largest magnitude.  Blocks of zeros (and those whose scale would be subnormal) get the smallest
-// normal number, so that its reciprocal is finite; a block that holds an infinity or NaN gets that as its scale.
+// What becomes 448: the largest magnitude of a block, at least 448 * 2^-126 (blocks of zeros, and those whose scale would be subnormal).
+__device__ __forceinline__ float block_top(unsigned largest) { return __uint_as_float(max(largest, 0x04e00000u)); }
+// The scale of a block: a normal number, so that its reciprocal is finite; a block that holds an infinity or NaN gets that as its scale.
 __device__ __forceinline__ float block_scale(unsigned largest)
 {
-    const unsigned least = 0x04e00000u;                 // 448 * 2^-126
-    const float top = __uint_as_float(max(largest, least)), t = top * (1.0f / kE4m3Max);
+    const float top = block_top(largest), t = top * (1.0f / kE4m3Max);
     const float s = fmaf(fmaf(-t, kE4m3Max, top), 1.0f / kE4m3Max, t);       // corrected by its remainder
     return largest < 0x7f800000u ? s : top;
 }
-// What an element is multiplied by to be in units of the scale.  The product's remainder corrects it (`in_units`), so that what is
-// rounded to e4m3 is the quotient as fp32 has it: without that one value in some ten thousand lands on the other side of a tie.
-__device__ __forceinline__ float per_scale(float scale)
+// What an element is multiplied by to be in units of the unrounded scale: 448 / max |x| = hi + lo to some 45 bits, so that x hi + x lo is rounded
+// once and a quotient that e4m3 holds, or that is a tie of it, comes out exactly.  Few digits make ties: by the rounded scale, one in twenty thousand
+// bf16 values fell on the wrong side of its tie; by its reciprocal alone one in some ten thousand of any.
+// (Beside an infinite value finite ones are zero.)
+struct Units { float hi, lo; };
+__device__ __forceinline__ Units block_units(unsigned largest, float scale)
 {
-    float y;
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(scale));
-    return y;
+    float hi;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(hi) : "f"(scale));
+    const float lo = fmaf(-hi, block_top(largest), kE4m3Max) * (hi * (1.0f / kE4m3Max));
+    return {hi, largest < 0x7f800000u ? lo : 0.0f};
 }
-// (scale: at most the largest finite number; beside an infinite one, finite values are zero)
-__device__ __forceinline__ void in_units(float (&y)[4], const float (&x)[4], float scale, float per)
+__device__ __forceinline__ void in_units(float (&y)[4], const float (&x)[4], Units u)
 {
-    const float p[4] = {per, per, per, per}, s[4] = {-scale, -scale, -scale, -scale};
-    float t[4], left[4];
-    mul_vec<4>(t, x, p);
-    fma_vec<4>(left, t, s, x);
-    fma_vec<4>(y, left, p, t);
+    const float hi[4] = {u.hi, u.hi, u.hi, u.hi}, lo[4] = {u.lo, u.lo, u.lo, u.lo};
+    float t[4];
+    mul_vec<4>(t, x, lo);
+    fma_vec<4>(y, x, hi, t);
 }
 // two values as e4m3, the nearest, at most 448 in magnitude
 __device__ __forceinline__ unsigned to_e4m3x2(float a, float b)
@@ -112,17 +114,15 @@ __device__ __forceinline__ void strip_magnitudes(const float (&y)[8], int lane, 
     }
 }
 
-// the lane's 8 elements, divided by their blocks' scales, as e4m3 bytes
+// the lane's 8 elements, in units of their blocks' scales, as e4m3 bytes
 template <int V>
-__device__ __forceinline__ void store_strip_e4m3(uint8_t *row, int c0, int width, int lane, const float (&x)[8], float s0, float s1)
+__device__ __forceinline__ void store_strip_e4m3(uint8_t *row, int c0, int width, int lane, const float (&x)[8], Units u0, Units u1)
 {
-    const float per0 = per_scale(s0), per1 = V == 8 ? per0 : per_scale(s1);
     const bool whole = c0 + kStrip <= width;
-    const float f0 = fminf(s0, 3.4028235e38f), f1 = fminf(s1, 3.4028235e38f);
     const float lo[4] = {x[0], x[1], x[2], x[3]}, hi[4] = {x[4], x[5], x[6], x[7]};
     float a[4], b[4];
-    in_units(a, lo, f0, per0);
-    in_units(b, hi, V == 8 ? f0 : f1, per1);
+    in_units(a, lo, u0);
+    in_units(b, hi, V == 8 ? u0 : u1);
     const float y[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
 #pragma unroll
     for (int q = 0; q < 8 / V; ++q) {
