@@ -403,7 +403,7 @@ enum { LSTM_BF16 = 2 };                      /* dtype of the operators' activati
  *   states: NULL, or fp32 [ceil(T / LSTM_LINREC_SEGMENT), B, D]: receives the state in front of processing step
  *   LSTM_LINREC_SEGMENT * k (behind a sequence's end, its last state); the backward pass reads it.
  * Decays above 1 are served as long as their product over the steps that count stays within the range of fp32; a state that
- * is infinite stays so or becomes NaN.
+ * is infinite stays so or becomes NaN, and so does every state behind a decay that is infinite or NaN.
  * T = 1 is the serving step: with hT = h0 the state is updated in place.
  * workspace: lstm_linear_recurrence_workspace(T, B, D) floats (0 for most sizes: then NULL will do; -1: bad sizes) that
  * nothing else uses until the call has run; the backward call needs as many.

@@ -265,7 +265,8 @@ __global__ void __launch_bounds__(kThreads, 4) linrec_forward_kernel(const __gri
             }
         }
 #pragma unroll
-        for (int v = 0; v < V; ++v) { m.A[v] = f[0][v]; m.H[v] = add[0][v]; }
+        for (int v = 0; v < V; ++v) m.A[v] = f[0][v];
+        first_added<V, GATE>(m.H, f[0], add[0]);
 #pragma unroll
         for (int k = 1; k < kSteps; ++k) {
             fma_vec<V>(m.H, f[k], m.H, add[k]);

@@ -71,9 +71,29 @@ __device__ __forceinline__ void apply(const Map<V> &m, float (&h)[V])
 {
     fma_vec<V>(h, m.A, h, m.H);
 }
-// m := later o m.  A product of decays that grew out of range is held at its edge: a state of zero stays zero behind it.
+// m := later o m.  A product of decays that grew out of range is held at its edge: a state of zero stays zero behind it.  A NaN stays
+// (fminf and fmaxf would take the edge in its place).
+__device__ __forceinline__ float within(float x, float edge)
+{
+    float y;
+    asm("{\n\t.reg .f32 e;\n\tneg.f32 e, %2;\n\tmin.NaN.f32 %0, %1, %2;\n\tmax.NaN.f32 %0, %0, e;\n\t}" : "=f"(y) : "f"(x), "f"(edge));
+    return y;
+}
 template <int V, bool GATE>
-__device__ __forceinline__ float held(float A) { return GATE ? A : fmaxf(-3.4028235e38f, fminf(3.4028235e38f, A)); }
+__device__ __forceinline__ float held(float A) { return GATE ? A : within(A, 3.4028235e38f); }
+// What a span's first step adds, from which its H starts.  A decay that is NaN or infinite makes it NaN: the state behind such a step is not
+// finite, whatever was in front of it, and by A alone, which is held, it could become so again.
+template <int V, bool GATE>
+__device__ __forceinline__ void first_added(float (&H)[V], const float (&f)[V], const float (&add)[V])
+{
+    const float zero[V] = {};
+    if (GATE) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) H[v] = add[v];
+    } else {
+        fma_vec<V>(H, f, zero, add);
+    }
+}
 template <int V, bool GATE>
 __device__ __forceinline__ void join_behind(Map<V> &m, const Map<V> &later)
 {

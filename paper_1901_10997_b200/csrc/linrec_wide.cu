@@ -210,7 +210,8 @@ __global__ void __launch_bounds__(Shape<T, V, false>::kThreads, Shape<T, V, fals
         in.next();
         float A[V], H[V];
 #pragma unroll
-        for (int v = 0; v < V; ++v) { A[v] = f[0][v]; H[v] = add[0][v]; }
+        for (int v = 0; v < V; ++v) A[v] = f[0][v];
+        first_added<V, GATE>(H, f[0], add[0]);
 #pragma unroll
         for (int k = 1; k < kSteps; ++k) {
             fma_vec<V>(H, f[k], H, add[k]);
