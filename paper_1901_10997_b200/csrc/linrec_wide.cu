@@ -423,7 +423,7 @@ __global__ void __launch_bounds__(64) linrec_short_kernel(const __grid_constant_
     }
 #pragma unroll
     for (int v = 0; v < V; ++v) h[v] = p.h0 ? p.h0[bd + v] : 0.0f;
-    if (p.states) store_vec<float, V>(p.states + bd, h);
+    if (p.states && p.T > 0) store_vec<float, V>(p.states + bd, h);      // (no steps: there are no saved states)
 #pragma unroll
     for (int k = 0; k < kShort; ++k) {
         if (k >= p.T) break;
