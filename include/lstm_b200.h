@@ -388,6 +388,7 @@ LSTM_API int lstm_forward_noalloc(const float *wx, const float *wh, const float 
  *   - strides (..._t, ..._b, ..._ld) count elements; the last dimension is contiguous.  Pointers are aligned to
  *     their elements.  Rows that are aligned to 16 bytes (widths of a multiple of 8) are read fastest.
  *   - outputs must not overlap inputs or each other, but for hT over h0 (and dh0 over dhT).
+ *     Strides by which an output would overlap itself are refused.
  *   - err (may be NULL): buffer of errlen bytes for the reason of a failure; nothing is launched then.
  * ------------------------------------------------------------------------------------------------- */
 enum { LSTM_BF16 = 2 };                      /* dtype of the operators' activations, beside LSTM_F32 */

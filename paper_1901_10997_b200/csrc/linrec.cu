@@ -596,6 +596,7 @@ int lstm_linear_recurrence(const void *a, long long a_t, long long a_b, const vo
     if (!aligned(a, dtype) || !aligned(x, dtype) || !aligned(h, dtype) || !aligned(h0, LSTM_F32) || !aligned(hT, LSTM_F32) ||
         !aligned(states, LSTM_F32) || !aligned(lengths, LSTM_F32))
         return fail(LSTM_ERR_INVALID, "bad argument: a pointer is not aligned to its elements");
+    if (!steps_apart(T, B, D, h_t, h_b)) return fail(LSTM_ERR_INVALID, "bad argument: rows of an output overlap");
     if (B == 0 || (T == 0 && !hT)) return LSTM_OK;
     LinrecArgs p = {};
     p.a = a; p.a_t = a_t; p.a_b = a_b;
@@ -622,6 +623,7 @@ int lstm_linear_recurrence_backward(const void *a, long long a_t, long long a_b,
     if (!aligned(a, dtype) || !aligned(x, dtype) || !aligned(dh, dtype) || !aligned(da, dtype) || !aligned(dx, dtype) ||
         !aligned(states, LSTM_F32) || !aligned(dhT, LSTM_F32) || !aligned(dh0, LSTM_F32) || !aligned(lengths, LSTM_F32))
         return fail(LSTM_ERR_INVALID, "bad argument: a pointer is not aligned to its elements");
+    if (!steps_apart(T, B, D, da_t, da_b) || !steps_apart(T, B, D, dx_t, dx_b)) return fail(LSTM_ERR_INVALID, "bad argument: rows of an output overlap");
     if (B == 0 || (T == 0 && !dh0)) return LSTM_OK;
     LinrecArgs p = {};
     p.a = a; p.a_t = a_t; p.a_b = a_b;

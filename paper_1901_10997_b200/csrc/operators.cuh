@@ -161,6 +161,25 @@ __device__ __forceinline__ void add_vec(float (&d)[V], const float (&a)[V], cons
             : "=f"(d[v]), "=f"(d[v + 1]) : "f"(a[v]), "f"(a[v + 1]), "f"(b[v]), "f"(b[v + 1]));
 }
 
+// rows of an output share no element
+inline bool rows_apart(int rows, int width, long long ld) { return rows < 2 || ld >= width || ld <= -(long long)width; }
+// ... nor do the runs of D elements of an output [T][B][D]: none begins within another
+inline bool steps_apart(int T, int B, int D, long long t, long long b)
+{
+    t = t < 0 ? -t : t;
+    b = b < 0 ? -b : b;
+    if (T < 2 || B < 2) return (T < 2 || t >= D) && (B < 2 || b >= D);
+    if (t < D || b < D) return false;
+    if (t < b) { const long long s = t; t = b; b = s; const int n = T; T = B; B = n; }
+    if ((t - D) / b >= B - 1) return true;              // the inner ones all lie between two of the outer
+    for (long long j = 1; j < B; ++j)                   // strides that cross (of either sign): is j b within D of a multiple of t?
+        for (long long i = j * b / t; i <= j * b / t + 1 && i < T; ++i) {
+            const long long off = j * b - i * t;
+            if (off < D && off > -D) return false;
+        }
+    return true;
+}
+
 inline bool known_type(int dtype) { return dtype == LSTM_F32 || dtype == LSTM_BF16; }
 inline int bytes_of(int dtype) { return dtype == LSTM_BF16 ? 2 : 4; }
 inline bool aligned_to(const void *p, int bytes) { return (uintptr_t)p % (unsigned)bytes == 0; }

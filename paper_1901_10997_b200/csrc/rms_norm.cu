@@ -319,6 +319,7 @@ int lstm_rms_norm(const void *x, long long x_ld, const void *residual, long long
         return fail(LSTM_ERR_INVALID, "bad argument: a pointer is not aligned to its elements");
     if (scales && (!aligned_to(y, 16) || y_ld % 16))
         return fail(LSTM_ERR_INVALID, "bad argument: 8-bit rows must start on 16 bytes");
+    if (!rows_apart(rows, width, y_ld) || (r && !rows_apart(rows, width, r_ld))) return fail(LSTM_ERR_INVALID, "bad argument: rows of an output overlap");
     int sms = 0;
     if (const int rc = device_sms(sms, fail)) return rc;
     RowAlignment al(width);
@@ -345,6 +346,7 @@ int lstm_rms_norm_backward(const void *dy, long long dy_ld, const void *r, long 
     if (!aligned_to(dy, es) || !aligned_to(r, es) || !aligned_to(dr, es) || !aligned_to(dx, es) || !aligned_to(w, 4) || !aligned_to(dw, 4) ||
         !aligned_to(workspace, 4))
         return fail(LSTM_ERR_INVALID, "bad argument: a pointer is not aligned to its elements");
+    if (!rows_apart(rows, width, dx_ld)) return fail(LSTM_ERR_INVALID, "bad argument: rows of an output overlap");
     int sms = 0;
     if (const int rc = device_sms(sms, fail)) return rc;
     const cudaStream_t st = (cudaStream_t)cuda_stream;
