@@ -6,16 +6,18 @@ fp8_quantize, fp8_product                        8-bit matrices with a scale for
 
 Tensors are CUDA tensors of one device; activations are bf16 or fp32 (all of a call of one type), states, scales, norm weights
 and biases fp32.  Only the last dimension has to be contiguous, unless said otherwise.  Every call enqueues kernels on torch's
-current stream of that device and returns; outputs are new tensors unless an ``out`` is taken.  Calls that cannot be served raise
-ValueError (the tensors) or LstmError (what the library refused).
+current stream of that device and returns; outputs are new tensors unless an ``out`` is taken, which may share no element with
+an input.  Calls that cannot be served raise ValueError (the tensors) or LstmError (what the library refused).
 
 A step of generation makes a few of these calls, each of a few microseconds on the GPU, so the checks here are few and plain.
 """
 from __future__ import annotations
 
 import ctypes
+import math
 import threading
 
+import numpy as np
 import torch
 
 from . import binding as _b
@@ -110,6 +112,46 @@ def _apart(t, name):
         reach += stride * (size - 1)
 
 
+def _runs(t):
+    """The addresses at which a tensor's runs of contiguous elements begin, in order, and their bytes."""
+    es, starts = t.element_size(), np.zeros(1, dtype=np.int64)
+    for size, stride in zip(t.shape[:-1], t.stride()[:-1]):
+        starts = (starts[:, None] + np.arange(size if stride else 1, dtype=np.int64) * (stride * es)).reshape(-1)
+    return np.sort(starts) + t.data_ptr(), t.shape[-1] * es
+
+
+def _share(out, t):
+    """Is an element of ``out`` (none of which overlap) also one of ``t``?"""
+    run, other = out.shape[-1] * out.element_size(), t.shape[-1] * t.element_size()
+    # runs at a common distance, those of one beside those of the other (halves of one matrix)
+    pitch = math.gcd(*(st * v.element_size() for v in (out, t) for st, n in zip(v.stride()[:-1], v.shape) if n > 1))
+    if pitch:
+        at = (out.data_ptr() - t.data_ptr()) % pitch
+        if at >= other and at + run <= pitch:
+            return False
+    begin, run = _runs(out)
+    theirs, other = _runs(t)
+    last = np.searchsorted(begin, theirs + other) - 1              # the last of out's runs that begins in front of the end of each
+    return bool(((last >= 0) & (begin[last] + run > theirs)).any())
+
+
+def _no_input(out, name, *inputs):
+    """``out`` shares no element with the inputs (tensors or None, each with its name)."""
+    if not out.numel():
+        return
+    at, end = _range(out)
+    for t, other in inputs:
+        if t is not None and t.numel():
+            begin, stop = _range(t)
+            if begin < end and at < stop and _share(out, t):
+                raise ValueError(f"{name} overlaps {other}")
+
+
+def _range(t):
+    at = t.data_ptr()
+    return at, at + (sum([(n - 1) * st for n, st in zip(t.shape, t.stride())]) + 1) * t.element_size()
+
+
 # ---------------------------------------------------------------- recurrence
 def _workspace(T, B, D, device):
     """A call's workspace, or None.  It is held until the call has been enqueued; torch's allocator orders its next use behind that."""
@@ -123,28 +165,41 @@ def linear_recurrence(a, x, h0=None, lengths=None, *, gate=True, reverse=False, 
     a, x: [T, B, D]; h0: fp32 [B, D] or None (zeros); lengths: int32 [B] on the device or None; ``reverse``: every sequence from its
     last step to its first.  Returns (h, hT, states): h [T, B, D] (zero behind a sequence's end), hT fp32 [B, D] the state behind
     the last step, states fp32 [ceil(T / 16), B, D] for the backward pass with ``save``, else None.  ``out``: a tensor for h;
-    ``state``: a contiguous one for hT, which may be h0 itself (a step of generation updates its state in place)."""
+    ``state``: a contiguous one for hT, which may be h0 itself (a step of generation updates its state in place) but no part of
+    another tensor of the call."""
     dev, dt = _first(a, "a")
     shape, dtype, device = a.shape, a.dtype, a.device
     T, B, D = shape
     rows = (B, D)
     pa, (a_t, a_b, _) = _ptr(a, "a", shape, dtype, dev)
     px, (x_t, x_b, _) = _ptr(x, "x", shape, dtype, dev)
+    out_given, state_given = out is not None, state is not None
     if out is None:
         out = _empty(shape, dtype=dtype, device=device)
         po, o_t, o_b = out.data_ptr(), B * D, D
     else:
-        _apart(out, "out")
         po, (o_t, o_b, _) = _ptr(out, "out", shape, dtype, dev)
+        _apart(out, "out")
     if state is None:
         state = _empty(rows, dtype=_F32, device=device)
         ps = state.data_ptr()
     else:
         ps = _whole(state, "state", rows, _F32, dev)
+    ph = 0 if h0 is None else ps if h0 is state else _whole(h0, "h0", rows, _F32, dev)
+    pl = 0 if lengths is None else _whole(lengths, "lengths", (B,), _I32, dev)
+    if out_given or state_given:            # ranges of addresses first; only where two meet does it matter which elements lie in them
+        es, n, m = 2 if dt == _b.LSTM_BF16 else 4, 4 * B * D, 4 * B
+        ea = pa + es * ((T - 1) * a_t + (B - 1) * a_b + D)
+        ex = px + es * ((T - 1) * x_t + (B - 1) * x_b + D)
+        eo = po + es * ((T - 1) * o_t + (B - 1) * o_b + D)
+        if out_given and (pa < eo and po < ea or px < eo and po < ex or ph < eo and po < ph + n or pl < eo and po < pl + m or ps < eo and po < ps + n):
+            _no_input(out, "out", (a, "a"), (x, "x"), (h0, "h0"), (lengths, "lengths"), (state, "state"))
+        end = ps + n
+        if state_given and (pa < end and ps < ea or px < end and ps < ex or ph != ps and ph < end and ps < ph + n or pl < end and ps < pl + m):
+            _no_input(state, "state", (a, "a"), (x, "x"), (None if ph == ps else h0, "h0"), (lengths, "lengths"))
     states = _empty((-(-T // LSTM_LINREC_SEGMENT), B, D), dtype=_F32, device=device) if save else None
     work = _workspace(T, B, D, device) if T > 64 else None
-    _call("lstm_linear_recurrence", dev, pa, a_t, a_b, px, x_t, x_b, 0 if h0 is None else ps if h0 is state else _whole(h0, "h0", rows, _F32, dev),
-          0 if lengths is None else _whole(lengths, "lengths", (B,), _I32, dev), T, B, D, dt,
+    _call("lstm_linear_recurrence", dev, pa, a_t, a_b, px, x_t, x_b, ph, pl, T, B, D, dt,
           (LSTM_LINREC_GATE if gate else 0) | (LSTM_LINREC_REVERSE if reverse else 0), po, o_t, o_b, ps, 0 if states is None else states.data_ptr(),
           0 if work is None else work.data_ptr(), 0 if work is None else work.numel())
     return out, state, states
@@ -273,13 +328,17 @@ def fp8_product(qx, sx, qw, sw, bias=None, *, dtype=torch.bfloat16, out=None):
     blocks = (width + 127) // 128
     px, (x_ld, _) = _ptr(qx, "qx", (rows, width), _E4M3, dev)
     pw, (w_ld, _) = _ptr(qw, "qw", (outs, width), _E4M3, dev)
+    ps, pt, pb = _whole(sx, "sx", (rows, blocks), _F32, dev), _whole(sw, "sw", ((outs + 127) // 128, blocks), _F32, dev), _whole(bias, "bias", (outs,), _F32, dev)
     if out is None:
         out = _empty((rows, outs), dtype=dtype, device=qx.device)
         po, o_ld = out.data_ptr(), outs
     else:
-        _apart(out, "out")
         po, (o_ld, _) = _ptr(out, "out", (rows, outs), dtype, dev)
+        _apart(out, "out")
+        end = po + (2 if dt == _b.LSTM_BF16 else 4) * ((rows - 1) * o_ld + outs)
+        if (px < end and po < px + (rows - 1) * x_ld + width or pw < end and po < pw + (outs - 1) * w_ld + width or pb < end and po < pb + 4 * outs or
+                ps < end and po < ps + 4 * rows * blocks or pt < end and po < pt + 4 * blocks * ((outs + 127) // 128)):
+            _no_input(out, "out", (qx, "qx"), (sx, "sx"), (qw, "qw"), (sw, "sw"), (bias, "bias"))
     one = (width + 15) // 16 * 16           # a single row is any distance from the next
-    _call("lstm_fp8_product", dev, px, x_ld if rows > 1 else one, _whole(sx, "sx", (rows, blocks), _F32, dev), pw, w_ld if outs > 1 else one,
-          _whole(sw, "sw", ((outs + 127) // 128, blocks), _F32, dev), _whole(bias, "bias", (outs,), _F32, dev), rows, outs, width, dt, po, o_ld)
+    _call("lstm_fp8_product", dev, px, x_ld if rows > 1 else one, ps, pw, w_ld if outs > 1 else one, pt, pb, rows, outs, width, dt, po, o_ld)
     return out
