@@ -465,7 +465,8 @@ LSTM_API int lstm_rms_norm_backward(const void *dy, long long dy_ld, const void 
  *     scale = max |x| / 448 over the block, at least the smallest normal number;   q = x / scale, the nearest, ties to even
  * (the quotient by the unrounded scale, as fp32 has it: ties are those of 448 x / max |x|).
  * A block that holds an infinity or a NaN gets that as its scale.  q rows start on 16 bytes (q and q_ld are multiples of
- * 16); the bytes between width and q_ld are left as they are.
+ * 16); the bytes between width and q_ld are left as they are.  LSTM_ERR_UNSUPPORTED: width above 2^31 - 4096 (65535 x 1024 with
+ * block_rows 1), more than 65535 blocks of 128 rows with block_rows 128.
  */
 LSTM_API int lstm_fp8_quantize(const void *x, long long x_ld, int rows, int width, int dtype, int block_rows, void *q, long long q_ld,
                                float *scales, void *cuda_stream, char *err, int errlen);
@@ -476,7 +477,7 @@ LSTM_API int lstm_fp8_quantize(const void *x, long long x_ld, int rows, int widt
  * qx [rows, width] with sx of block_rows 1, qw [outs, width] with sw of block_rows 128 (rows start on 16 bytes),
  * bias [outs] fp32 or NULL, y [rows, outs] of dtype.  Products run on the tensor cores (tcgen05, e4m3 operands); the sum
  * of a block of 128 columns is scaled and added up in fp32.  A wait inside the kernel that gives up (which only a failed
- * device can cause) leaves NaN in its tile of y.
+ * device can cause) leaves NaN in its tile of y.  LSTM_ERR_UNSUPPORTED: outs or width above 2^31 - 4096, more than 65535 x 128 rows.
  */
 LSTM_API int lstm_fp8_product(const void *qx, long long qx_ld, const float *sx, const void *qw, long long qw_ld, const float *sw,
                               const float *bias, int rows, int outs, int width, int dtype, void *y, long long y_ld,

@@ -638,6 +638,7 @@ extern "C" int lstm_fp8_product(const void *qx, long long qx_ld, const float *sx
     if (!aligned_to(qx, 16) || !aligned_to(qw, 16) || qx_ld % 16 || qw_ld % 16 || qx_ld < width || qw_ld < width)
         return fail(LSTM_ERR_INVALID, "bad argument: 8-bit rows must start on 16 bytes and not overlap");
     if (!rows_apart(rows, outs, y_ld)) return fail(LSTM_ERR_INVALID, "bad argument: rows of an output overlap");
+    if (outs > kMostColumns || width > kMostColumns) return fail(LSTM_ERR_UNSUPPORTED, "rows of more than 2^31 - 4096 columns");
     if (rows > 65535 * 128) return fail(LSTM_ERR_UNSUPPORTED, "more than 65535 tiles of rows");
     int sms = 0;
     if (const int rc = device_sms(sms, fail)) return rc;

@@ -144,6 +144,7 @@ extern "C" int lstm_fp8_quantize(const void *x, long long x_ld, int rows, int wi
     if (!aligned_to(q, 16) || q_ld % 16) return fail(LSTM_ERR_INVALID, "bad argument: 8-bit rows must start on 16 bytes");
     if (!rows_apart(rows, width, q_ld)) return fail(LSTM_ERR_INVALID, "bad argument: rows of an output overlap");
     if (block_rows == 128 && (rows + 127ll) / 128 > 65535) return fail(LSTM_ERR_UNSUPPORTED, "more than 65535 blocks of rows");
+    if (width > kMostColumns) return fail(LSTM_ERR_UNSUPPORTED, "rows of more than 2^31 - 4096 columns");
     if (block_rows == 1 && (width + 1023ll) / 1024 > 65535) return fail(LSTM_ERR_UNSUPPORTED, "rows of more than 65535 x 1024 columns");
     int sms = 0;
     if (const int rc = device_sms(sms, fail)) return rc;

@@ -180,6 +180,7 @@ inline bool steps_apart(int T, int B, int D, long long t, long long b)
     return true;
 }
 
+constexpr int kMostColumns = 0x7ffff000;                 // of a row: the end of its last strip, block or tile is still counted in 32 bits
 inline bool known_type(int dtype) { return dtype == LSTM_F32 || dtype == LSTM_BF16; }
 inline int bytes_of(int dtype) { return dtype == LSTM_BF16 ? 2 : 4; }
 inline bool aligned_to(const void *p, int bytes) { return (uintptr_t)p % (unsigned)bytes == 0; }

@@ -103,6 +103,14 @@ def _whole(t, name, shape, dtype, device):
     raise ValueError(f"{name} must be contiguous {dtype} {tuple(shape)} on cuda:{device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
 
 
+# the library counts in 32 bits, and ctypes would cut off what is above
+_MOST = 0x7fffffff
+
+
+def _too_large():
+    raise ValueError("dimensions of 2^31 and more are not served")
+
+
 def _apart(t, name):
     """Outputs that are written: no two elements of them may be one."""
     reach = t.shape[-1] if t.dim() else 0
@@ -170,6 +178,8 @@ def linear_recurrence(a, x, h0=None, lengths=None, *, gate=True, reverse=False, 
     dev, dt = _first(a, "a")
     shape, dtype, device = a.shape, a.dtype, a.device
     T, B, D = shape
+    if T > _MOST or B > _MOST or D > _MOST:
+        _too_large()
     rows = (B, D)
     pa, (a_t, a_b, _) = _ptr(a, "a", shape, dtype, dev)
     px, (x_t, x_b, _) = _ptr(x, "x", shape, dtype, dev)
@@ -211,6 +221,8 @@ def linear_recurrence_backward(a, x, states, dh, dhT=None, lengths=None, *, gate
     dev, dt = _first(a, "a")
     shape, dtype, device = a.shape, a.dtype, a.device
     T, B, D = shape
+    if T > _MOST or B > _MOST or D > _MOST:
+        _too_large()
     rows = (B, D)
     pa, (a_t, a_b, _) = _ptr(a, "a", shape, dtype, dev)
     px, (x_t, x_b, _) = _ptr(x, "x", shape, dtype, dev)
@@ -230,10 +242,13 @@ def linear_recurrence_backward(a, x, states, dh, dhT=None, lengths=None, *, gate
 # ---------------------------------------------------------------- norm
 def _matrix(x, name):
     dev, dt = _first(x, name)
-    if x.dim() != 2:
+    shape = x.shape
+    if len(shape) != 2:
         raise ValueError(f"{name} must be a matrix")
-    px, (ld, _) = _ptr(x, name, x.shape, x.dtype, dev)
-    return dev, dt, x.shape, px, ld
+    if shape[0] > _MOST or shape[1] > _MOST:
+        _too_large()
+    px, (ld, _) = _ptr(x, name, shape, x.dtype, dev)
+    return dev, dt, shape, px, ld
 
 
 def _norm(dev, dt, shape, px, x_ld, x, weight, residual, eps, y, y_ld, scales):
@@ -320,6 +335,8 @@ def fp8_product(qx, sx, qw, sw, bias=None, *, dtype=torch.bfloat16, out=None):
         raise ValueError("qx and qw must be CUDA matrices") from None
     if dev < 0:
         raise ValueError("the library works on CUDA tensors")
+    if rows > _MOST or outs > _MOST or width > _MOST:
+        _too_large()
     dt = _TYPES.get(dtype)
     if dt is None:
         raise ValueError(f"dtype must be bf16 or fp32, got {dtype}")
