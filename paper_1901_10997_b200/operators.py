@@ -7,7 +7,8 @@ fp8_quantize, fp8_product                        8-bit matrices with a scale for
 Tensors are CUDA tensors of one device; activations are bf16 or fp32 (all of a call of one type), states, scales, norm weights
 and biases fp32.  Only the last dimension has to be contiguous, unless said otherwise.  Every call enqueues kernels on torch's
 current stream of that device and returns; outputs are new tensors unless an ``out`` is taken, which may share no element with
-an input.  Calls that cannot be served raise ValueError (the tensors) or LstmError (what the library refused).
+an input.  Calls that cannot be served raise ValueError (the tensors) or LstmError (what the library refused).  The calls record no graph: gradients are calls of their own, and
+while torch records gradients, tensors that require them are refused.
 
 A step of generation makes a few of these calls, each of a few microseconds on the GPU, so the checks here are few and plain.
 """
@@ -101,6 +102,15 @@ def _whole(t, name, shape, dtype, device):
     except AttributeError:
         raise ValueError(f"{name} must be a CUDA tensor") from None
     raise ValueError(f"{name} must be contiguous {dtype} {tuple(shape)} on cuda:{device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+
+
+_recording = torch.is_grad_enabled
+
+
+def _no_graph():
+    """No gradient is lost without a word."""
+    raise ValueError("this call records no graph for a tensor that requires gradients: call it under torch.no_grad() or detach the tensor "
+                     "(linear_recurrence_backward and rms_norm_backward compute gradients)")
 
 
 # the library counts in 32 bits, and ctypes would cut off what is above
@@ -207,6 +217,8 @@ def linear_recurrence(a, x, h0=None, lengths=None, *, gate=True, reverse=False, 
         end = ps + n
         if state_given and (pa < end and ps < ea or px < end and ps < ex or ph != ps and ph < end and ps < ph + n or pl < end and ps < pl + m):
             _no_input(state, "state", (a, "a"), (x, "x"), (None if ph == ps else h0, "h0"), (lengths, "lengths"))
+    if _recording() and (a.requires_grad or x.requires_grad or h0 is not None and h0.requires_grad or out.requires_grad or state.requires_grad):
+        _no_graph()
     states = _empty((-(-T // LSTM_LINREC_SEGMENT), B, D), dtype=_F32, device=device) if save else None
     work = _workspace(T, B, D, device) if T > 64 else None
     _call("lstm_linear_recurrence", dev, pa, a_t, a_b, px, x_t, x_b, ph, pl, T, B, D, dt,
@@ -229,11 +241,14 @@ def linear_recurrence_backward(a, x, states, dh, dhT=None, lengths=None, *, gate
     pd, (d_t, d_b, _) = _ptr(dh, "dh", shape, dtype, dev)
     if states is None:
         raise ValueError("states must be those that linear_recurrence saved")
+    ph, pl = _whole(dhT, "dhT", rows, _F32, dev), _whole(lengths, "lengths", (B,), _I32, dev)
+    if _recording() and (a.requires_grad or x.requires_grad or dh.requires_grad or dhT is not None and dhT.requires_grad):
+        _no_graph()
     da, dx = _empty(shape, dtype=dtype, device=device), _empty(shape, dtype=dtype, device=device)
     dh0 = _empty(rows, dtype=_F32, device=device)
     work = _workspace(T, B, D, device) if T > 64 else None
     _call("lstm_linear_recurrence_backward", dev, pa, a_t, a_b, px, x_t, x_b, _whole(states, "states", (-(-T // LSTM_LINREC_SEGMENT), B, D), _F32, dev),
-          pd, d_t, d_b, _whole(dhT, "dhT", rows, _F32, dev), _whole(lengths, "lengths", (B,), _I32, dev), T, B, D, dt,
+          pd, d_t, d_b, ph, pl, T, B, D, dt,
           (LSTM_LINREC_GATE if gate else 0) | (LSTM_LINREC_REVERSE if reverse else 0), da.data_ptr(), B * D, D, dx.data_ptr(), B * D, D, dh0.data_ptr(),
           0 if work is None else work.data_ptr(), 0 if work is None else work.numel())
     return da, dx, dh0
@@ -261,8 +276,10 @@ def _norm(dev, dt, shape, px, x_ld, x, weight, residual, eps, y, y_ld, scales):
         pr = r.data_ptr()
     if weight is None:
         raise ValueError("weight must be a CUDA tensor")
-    _call("lstm_rms_norm", dev, px, x_ld, pres, res_ld, _whole(weight, "weight", (width,), _F32, dev), eps, rows, width, dt, y.data_ptr(), y_ld, scales, pr,
-          width)
+    pw = _whole(weight, "weight", (width,), _F32, dev)
+    if _recording() and (x.requires_grad or weight.requires_grad or residual is not None and residual.requires_grad):
+        _no_graph()
+    _call("lstm_rms_norm", dev, px, x_ld, pres, res_ld, pw, eps, rows, width, dt, y.data_ptr(), y_ld, scales, pr, width)
     return r
 
 
@@ -304,12 +321,14 @@ def rms_norm_backward(dy, r, weight, dr=None, *, eps=1e-6):
         pd, (d_ld, _) = _ptr(dr, "dr", shape, r.dtype, dev)
     if weight is None:
         raise ValueError("weight must be a CUDA tensor")
+    pw = _whole(weight, "weight", (width,), _F32, dev)
+    if _recording() and (dy.requires_grad or r.requires_grad or weight.requires_grad or dr is not None and dr.requires_grad):
+        _no_graph()
     dx = _empty(shape, dtype=r.dtype, device=r.device)
     dw = _empty((width,), dtype=_F32, device=r.device)
     need = _norm_workspace(dev, rows, width)
     work = _empty((need,), dtype=_F32, device=r.device)
-    _call("lstm_rms_norm_backward", dev, py, y_ld, pr, r_ld, _whole(weight, "weight", (width,), _F32, dev), pd, d_ld, eps, rows, width, dt, dx.data_ptr(), width,
-          dw.data_ptr(), work.data_ptr(), need)
+    _call("lstm_rms_norm_backward", dev, py, y_ld, pr, r_ld, pw, pd, d_ld, eps, rows, width, dt, dx.data_ptr(), width, dw.data_ptr(), work.data_ptr(), need)
     return dx, dw
 
 
@@ -318,6 +337,8 @@ def fp8_quantize(x, *, block_rows=1):
     """x [rows, width] as (q, scales) with x ~ scale * q: a scale for each 128 columns of a row (``block_rows`` 1: activations,
     scales [rows, ceil(width / 128)]) or for each 128 x 128 block (128: weights, scales [ceil(rows / 128), ceil(width / 128)])."""
     dev, dt, (rows, width), px, x_ld = _matrix(x, "x")
+    if _recording() and x.requires_grad:
+        _no_graph()
     ld = (width + 15) // 16 * 16
     held = _empty((rows, ld), dtype=_E4M3, device=x.device)
     scales = _empty(((rows + block_rows - 1) // block_rows if block_rows > 0 else 0, (width + 127) // 128), dtype=_F32, device=x.device)
@@ -356,6 +377,8 @@ def fp8_product(qx, sx, qw, sw, bias=None, *, dtype=torch.bfloat16, out=None):
         if (px < end and po < px + (rows - 1) * x_ld + width or pw < end and po < pw + (outs - 1) * w_ld + width or pb < end and po < pb + 4 * outs or
                 ps < end and po < ps + 4 * rows * blocks or pt < end and po < pt + 4 * blocks * ((outs + 127) // 128)):
             _no_input(out, "out", (qx, "qx"), (sx, "sx"), (qw, "qw"), (sw, "sw"), (bias, "bias"))
+    if _recording() and (sx.requires_grad or sw.requires_grad or bias is not None and bias.requires_grad or out.requires_grad):
+        _no_graph()
     one = (width + 15) // 16 * 16           # a single row is any distance from the next
     _call("lstm_fp8_product", dev, px, x_ld if rows > 1 else one, ps, pw, w_ld if outs > 1 else one, pt, pb, rows, outs, width, dt, po, o_ld)
     return out
