@@ -479,34 +479,38 @@ cudaError_t by_vector(LinrecArgs &p, int v, bool backward, cudaStream_t st)
 
 }  // namespace
 
+// From here on vectors of two channels, or of one, make some 1.2 CTAs an SM (of 148) by themselves: many channels, without chunks.
+static long long many_channels(int v) { return v == 1 ? 5600 : 11000; }
+
 // Chunks pay where channels alone do not fill the chip and the work is large enough for a second launch and a second reading, most of
 // which comes from L2 up to some ten million elements.  us, cluster of CTAs (linrec.cu) / chunks: 65536 x 1 x 1500 of bf16 261 / 200,
 // backward 529 / 320; 16384 x 1 x 1500 69 / 59; 4096 x 4 x 1000 52 / 41; 65536 x 1 x 256 102 / 48; 4096 x 1 x 1500 20 / 21.
-// As many chunks as make some 75000 channels side by side, just under what is resident at once (65536 x 1500: 36000 228 us, 48000 200, 93000
-// 194, 120000 217; backward 342, 320, 336, 340, and 72000 295), and no more than 64: each has to run through the maps of those before it.
+// As many chunks as make some 75000 channels side by side, just under what is resident at once in vectors of four bf16 (65536 x 1500: 36000 228 us, 48000
+// 200, 93000 194, 120000 217; backward 342, 320, 336, 340, and 72000 295); fp32 in vectors of two makes several waves of them.  No more than 64: each
+// has to run through the maps of those before it.
 int linrec_chunks(int T, int B, int D, int &chunk_len)
 {
     chunk_len = T;
     const long long channels = (long long)B * D;
-    // from here on vectors of two channels, or of one, make more than one CTA an SM by themselves (linrec_wide_serves)
-    if (channels > (D % 2 ? 5600 : 11000) || channels * T < 8000000 || T < 512) return 1;
+    if (channels > many_channels(D % 2 ? 1 : 2) || channels * T < 8000000 || T < 512) return 1;
     const int want = (int)std::min(std::max(75000 / channels, 2ll), 64ll);
     const long long len = (((long long)T + want - 1) / want + 63) / 64 * 64;
     chunk_len = (int)len;
     return (int)((T + len - 1) / len);
 }
 
-// Without chunks: where vectors of four make two CTAs an SM, else with vectors of two where those make more than one.  us, linrec.cu / here:
-// 2048 x 32 x 1500 of bf16 165 / 108, 400 x 64 x 800 45 / 29, 35 x 20 x 1500 9.6 / 5.5, 512 x 64 x 1501 103 / 78, 4096 x 8 x 1500 of fp32 130 / 112 (188
-// CTAs of vectors of two; with vectors of four, 94 CTAs, 148); below the line 400 x 16 x 800 of bf16 13.8 / 14.7, 200 x 8 x 700 7.2 / 8.2.
+// Without chunks: vectors of four where they make two CTAs an SM, else of two (or one), from many_channels on.  us, linrec.cu / here: 2048 x 32 x 1500
+// of bf16 165 / 110, 400 x 64 x 800 47 / 25, 35 x 20 x 1500 8.7 / 4.9, 512 x 64 x 1501 131 / 77, 4096 x 8 x 1500 of fp32 132 / 113 (188 CTAs of vectors of
+// two; with vectors of four, 94 CTAs, 148).  Just above the line 16384 x 4 x 2800 338 / 306, of fp32 476 / 404, backward 682 / 641 and 1004 / 769; 400 x 14 x 800
+// 11.2 / 11.1, of fp32 backward 28 / 21; 400 x 7 x 801 13.8 / 12.1.  Bf16 gradients in vectors of one are the exception, 1000 x 7 x 809 46 / 50.  Below it
+// 400 x 12 x 800 11.1 / 11.1, of fp32 11.9 / 12.5, 200 x 8 x 700 6.5 / 6.3, and long sequences in chunks.
 bool linrec_wide_serves(const LinrecArgs &p, int v, bool bf16, bool backward, int sms, int &wide_v)
 {
     const long long channels = (long long)p.chunks * p.B * p.D;
-    auto groups = [&](int n) { return (channels / n + 31) / 32; };
     wide_v = bf16 ? v : std::min(v, 2);
     if (p.T <= kShort && !backward) return true;
-    if (wide_v == 4 && groups(4) < 2 * sms) wide_v = 2;
-    return p.chunks > 1 || groups(wide_v) * 5 >= 6ll * sms;
+    if (wide_v == 4 && (channels / 4 + 31) / 32 < 2 * sms) wide_v = 2;
+    return p.chunks > 1 || channels > (bf16 && backward && wide_v == 1 ? 5664 : many_channels(wide_v));
 }
 
 cudaError_t launch_linrec_wide(LinrecArgs &p, int v, bool bf16, bool backward, cudaStream_t st)
