@@ -438,6 +438,7 @@ LSTM_API int lstm_linear_recurrence_backward(const void *a, long long a_t, long 
  * x, residual, r [rows, width] of dtype (residual and r may be NULL), w [width] fp32.  scales NULL: y [rows, width] of
  * dtype.  scales not NULL: y holds e4m3 bytes (rows that start on 16 bytes) and scales [rows, ceil(width / 128)] as
  * lstm_fp8_quantize with block_rows 1 makes them from the unrounded y.  y is computed from the unrounded sum.
+ * The squares are summed in fp32: a row whose squares add up to more than its range (|r| of some 1e19) gives zeros.
  * width <= LSTM_RMS_NORM_MAX_WIDTH, else LSTM_ERR_UNSUPPORTED.
  */
 #define LSTM_RMS_NORM_MAX_WIDTH 16384
@@ -476,8 +477,10 @@ LSTM_API int lstm_fp8_quantize(const void *x, long long x_ld, int rows, int widt
  *     y[m,n] = sum_j sx[m,j] sw[n / 128, j] sum_{k in block j} qx[m,k] qw[n,k]  (+ bias[n])
  * qx [rows, width] with sx of block_rows 1, qw [outs, width] with sw of block_rows 128 (rows start on 16 bytes),
  * bias [outs] fp32 or NULL, y [rows, outs] of dtype.  Products run on the tensor cores (tcgen05, e4m3 operands); the sum
- * of a block of 128 columns is scaled and added up in fp32.  A wait inside the kernel that gives up (which only a failed
- * device can cause) leaves NaN in its tile of y.  LSTM_ERR_UNSUPPORTED: outs or width above 2^31 - 4096, more than 65535 x 128 rows.
+ * of a block of 128 columns is scaled and added up in fp32; where the product of two scales is below the normal range of fp32 its
+ * digits are lost.  Waits inside the kernel are for its own copies and instructions; one that lasts 4e9 clock ticks (about two seconds: a
+ * failed device, or one that other processes hold for as long) gives up and leaves NaN in its tile of y, as in the recurrence.
+ * No status says so: NaN from finite operands does.  LSTM_ERR_UNSUPPORTED: outs or width above 2^31 - 4096, more than 65535 x 128 rows.
  */
 LSTM_API int lstm_fp8_product(const void *qx, long long qx_ld, const float *sx, const void *qw, long long qw_ld, const float *sw,
                               const float *bias, int rows, int outs, int width, int dtype, void *y, long long y_ld,

@@ -287,7 +287,8 @@ cudaError_t launch_few(ProductArgs &p, const CUtensorMap &mw, const CUtensorMap 
 // Warps 0-15 read the accumulators back (quadrant = warp % 4, 64 columns each), warp 16 fetches, warp 17 of the first
 // CTA multiplies for both, warps 18 and 19 bring the scales of the rows of x, which lie a row's length apart, 16 blocks at a time into
 // shared memory (each reading warp on its own would touch 32 lines a block).
-// 25600 x 6400 x 1600 in 284 us: 1850 TFLOP/s, the tensor pipe 49 % active.  Of those 206 are operands and products (without reading
+// 25600 x 6400 x 1600 in 278 to 284 us: 1850 TFLOP/s, the tensor pipe 49 % active (in a burst; for seconds under the power cap 323, a bf16 product of
+// that size 357 and 412).  Of those 206 are operands and products (without reading
 // back), 50 the reading back, the rest the tiles' ends.  Steps: eight reading warps with 128 sums each 704 us, 16 with 64 410, scales staged and
 // results turned in shared memory 306, tensor copies of the results 284.
 // ---------------------------------------------------------------------------------------------------

@@ -1,6 +1,7 @@
 // 8-bit values (e4m3) with a scale for each 128 columns of a row, or for each 128 x 128 block: the largest magnitude of a block
 // becomes 448, q = x / scale rounded to the nearest.  Bound by memory; every element is read once and stays in registers between
-// the maximum and the rounding.  Rows: 25600 x 1312 of bf16 in 23.8 us, 0.66 of the copy rate; blocks: 5000 x 6000 in 20 us, 0.69.
+// the maximum and the rounding.  Rows: 25600 x 1312 of bf16 in 23.8 us, 0.66 of the copy rate, 73 % of the issue slots taken (17
+// instructions an element: maxima, conversions, addresses; two of them, in pairs, make the quotient); blocks: 5000 x 6000 in 20 us, 0.69.
 #include "../../include/lstm_b200.h"
 #include "row_parts.cuh"
 

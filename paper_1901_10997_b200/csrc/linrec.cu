@@ -486,8 +486,9 @@ cudaError_t launch(LinrecArgs &p, bool backward, int sms, cudaStream_t st)
     // warps of a CTA: no more than there are steps for
     const int warps = need >= kThreads / 32 ? kThreads / 32 : need > 1 ? (int)need : 1;
     // CTAs of a cluster: two for each SM, no more than there are steps for; 16 (which few places on the chip can hold) only
-    // where 8 do not reach every SM.  us by CTAs a cluster: 400 groups of channels (400 x 16 x 800 of fp32) 1: 14.6, 2: 21.7, 4: 27.7;
-    // 47 groups (65536 x 1500) 2: 561, 4: 405, 8: 278, 12: 389, 16: 495
+    // where 8 do not reach every SM.  us by CTAs a cluster, bf16: 47 groups of channels (4096 x 1 x 1500) 1: 53.6, 2: 34.6, 4: 24.9, 8: 20.4, 16: 32.4;
+    // 94 groups (1024 x 2 x 1500) 1: 15.1, 2: 12.8, 4: 10.0, 8: 13.2; 300 groups (400 x 12 x 800) 1: 11.0, 2: 15.5; 4 groups (65536 x 1 x 120) 8: 150, 16: 93.
+    // Gradients, of which fewer CTAs fit an SM, would be faster with half as many: 4096 x 1 x 1500 4: 33.5, 8: 38.3; 400 x 4 x 800 1: 8.5, 4: 12.7.
     int csize = 1;
     while (csize < kMaxCluster && groups * csize < (csize < 8 ? 2ll : 1ll) * sms && (long long)warps * csize < need) csize *= 2;
     p.csize = csize;

@@ -6,7 +6,7 @@
 //
 // Bound by memory: a row is read once into the registers of one warp (up to 512 columns) or of up to 16, summed by shuffles, and
 // written once.  Sums are fp32 over at most 32 elements a lane before they are joined pairwise.
-// Share of the copy rate, bf16: 25600 x 1500 with residual 0.98 (48 us), 25600 x 1600 to 8 bits 0.82 (54 us: 80 % of the issue slots taken),
+// Share of the copy rate, bf16: 25600 x 1500 with residual 0.98 (48 us), 25600 x 1600 to 8 bits 0.81 (54 us: 72 % of the issue slots taken),
 // gradients of 25600 x 1500 0.80 (58 us); rows that start anywhere (odd widths) are read two bytes at a time: 0.73, 0.56 and 0.43.
 #include "../../include/lstm_b200.h"
 #include "row_parts.cuh"
